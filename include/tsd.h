@@ -55,7 +55,8 @@ typedef enum {
   TSD_ERR_DEVICE_DATA = -6  /* a kernel met inconsistent device data (reported via status) */
 } tsd_error;
 
-typedef enum { TSD_F32 = 0, TSD_BF16 = 1 } tsd_dtype;
+/* TSD_E4M3 (8-bit codes: 1 sign, 4 exponent bits with bias 7, 3 mantissa bits, no infinities): pages of a paged cache only. */
+typedef enum { TSD_F32 = 0, TSD_BF16 = 1, TSD_E4M3 = 2 } tsd_dtype;
 
 /* Which draft blocks count as verified (Section 3.3).  EXACT: the rows and
  * tokens a child adds equal the set that threshold decoding would unmask at
@@ -610,6 +611,107 @@ int tsd_report_block(int32_t batch, const int32_t* n_masked, const uint32_t* sta
                      uint32_t ticket, tsd_stream_t stream);
 int tsd_wait_block(int32_t batch, const uint64_t* report, uint32_t ticket, int32_t* max_masked,
                    uint32_t* status_bits, tsd_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * A K/V cache in pages.  No counterpart in the paper, which keeps one dense cache per sequence; a server whose
+ * requests come and go keeps all of them in one pool and hands out pages of it.  Key t of sequence s is row
+ * t % page_size of page page_table[s, t / page_size].
+ *
+ *   k_pages, v_pages  device, 16-byte aligned: [n_pages, page_size, n_kv_heads, head_dim] of `dtype`, addressed
+ *                through page_stride (page, row, head; in elements, multiples of 16 bytes, shared by K and V, each
+ *                at least head_dim); head_dim contiguous.
+ *   k_scale, v_scale  device fp32 [n_kv_heads], nullable (= 1), for TSD_E4M3 only: a cached value is
+ *                decode(code) * scale[kv head].
+ *   page_table   device int32 [batch, max_pages], sequences table_stride entries apart.  Only the entries of
+ *                tokens that a call reads or writes are looked at.  One of those outside [0, n_pages) sets
+ *                TSD_STATUS_BAD_INDEX: its tokens are not written, and read as rows of zeros.
+ *   page_size    8, 16, 32, ... 1024;  max_pages * page_size < 2^31.
+ *   head_dim     64 or 128;  dtype TSD_F32, TSD_BF16 or TSD_E4M3 (with queries, new rows and outputs in bf16).
+ * Pages may be shared by sequences that only read them.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  void *k_pages, *v_pages;
+  int64_t page_stride[3];
+  const float *k_scale, *v_scale;
+  const int32_t* page_table;
+  int64_t table_stride;
+  int32_t batch, n_pages, page_size, max_pages, n_kv_heads, head_dim, dtype;
+} tsd_paged_cache;
+
+/* ---------------------------------------------------------------------------
+ * New rows into a paged cache, with the position rotation on the way (Appendix A: the dual cache is refreshed
+ * at block boundaries; and what tsd_gather_accepted_kv does for a dense cache).  Row i < n_new[s] of sequence s
+ * goes to slot t = first_slot[s] + i of its cache and stands at position p = positions[s, i], or t.  With
+ * a_j = p * inv_freq[j], j < rotary_dim / 2, every pair of dimensions (j, j + rotary_dim / 2), or (2j, 2j + 1)
+ * with `interleaved`, of its queries and keys becomes (x cos a - y sin a, x sin a + y cos a); dimensions from
+ * rotary_dim on and the values stay as they are.  Angles are taken in fp64, products in fp32; each result is
+ * rounded once, to the type it is stored in (TSD_E4M3: rn(x / scale), saturating at 448).
+ *
+ *   cache        nullable: rotate only (then k_out, or q and q_out, take the results; v is not read).
+ *   k, v         device [batch, n_blocks * n_rows, n_kv_heads, head_dim] of `dtype`, strides kv_stride (batch,
+ *                row, head); q likewise with n_q_heads, nullable.  The rows that count are those of block block[s] (nullable =
+ *                0): rows [block[s] * n_rows, + n_rows), e.g. those of the accepted node.
+ *   q_out, k_out device, rotated rows at the same places as in q and k; q_out with q, k_out nullable.  Each may
+ *                be its input (same strides), and otherwise must not overlap it.
+ *   n_new        device int32 [batch], nullable (= n_rows), clamped to [0, n_rows]: rows of each sequence that count.
+ *                What belongs to the others, in the cache and in q_out and k_out, is left as it was.
+ *   first_slot   device int32 [batch], nullable (= 0);  positions device int32 [batch, n_rows], nullable.
+ *   inv_freq     device fp32 [rotary_dim / 2];  rotary_dim a multiple of 16, 0 (no rotation) to head_dim.
+ * All bases 16-byte aligned, strides multiples of 16 bytes.  A block outside [0, n_blocks) sets TSD_STATUS_BAD_INDEX
+ * and leaves that sequence unwritten; so does a slot outside the cache, for that row of the cache.  Two rows that
+ * go to one slot (sequences that share the page) leave it with the bytes of either.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  const tsd_paged_cache* cache;
+  int32_t batch, n_blocks, n_rows, n_q_heads, n_kv_heads, head_dim, dtype;
+  const int32_t *block, *n_new, *first_slot, *positions;
+  const float* inv_freq;
+  int32_t rotary_dim, interleaved;
+  const void *k, *v, *q;
+  int64_t kv_stride[3], q_stride[3];
+  void *k_out, *q_out;
+  int64_t k_out_stride[3], q_out_stride[3];
+  uint32_t* status;
+} tsd_append_args;
+int tsd_append_paged_kv(const tsd_append_args* args, tsd_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Attention of one new token per sequence over its pages: for every sequence s and query head h
+ *     out[s, h] = sum_t softmax_t(sm_scale * <q[s, h], k_t>) v_t ,  t < kv_lens[s],
+ * kv head h / (n_q_heads / n_kv_heads).  The new token's own key and value are in the cache already.  A sequence
+ * of length 0 gives 0 and a log-sum-exp of -inf.  Rows at or past kv_lens[s] can hold anything.
+ *
+ *   q, out     device [batch, n_q_heads, head_dim] of `dtype` (TSD_F32 with an fp32 cache, else TSD_BF16), strides
+ *              (batch, head); 16-byte aligned bases and strides.
+ *   kv_lens    device int32 [batch], nullable (= max_pages * page_size), clamped to that.
+ *   lse        device fp32 [batch, n_q_heads], nullable: natural-log sum-exp of the scaled scores.
+ *   workspace  device, 16-byte aligned, tsd_paged_attention_workspace_bytes() bytes: parts of sequences that
+ *              several thread blocks share, and ticket words.  Zero it once before its first use; a completed call leaves every ticket
+ *              word at 0.  Two calls that may overlap on the GPU need a workspace each; other shapes may share one.
+ * The sequences' lengths together are cut evenly over the GPU, whatever the single ones are.
+ * ------------------------------------------------------------------------- */
+size_t tsd_paged_attention_workspace_bytes(const tsd_paged_cache* cache, int32_t n_q_heads);
+int tsd_paged_attention(const tsd_paged_cache* cache, int32_t n_q_heads, int32_t dtype, const void* q,
+                        int64_t q_stride_b, int64_t q_stride_head, const int32_t* kv_lens, void* out,
+                        int64_t o_stride_b, int64_t o_stride_head, float* lse, float sm_scale, void* workspace,
+                        size_t workspace_bytes, uint32_t* status, tsd_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * tsd_verify_attention with the cached keys and values read from pages: arguments as for that call, the cache's
+ * batch, kv heads and head_dim those of the layout, max_pages * page_size >= layout n_cache; the sequences' cached
+ * lengths are those of the mask.  bf16 pages are read in place by the tensor-core kernel (sm_scale > 0, else
+ * TSD_ERR_UNSUPPORTED).  8-bit pages (values bf16(decode(code) * scale), as for
+ * tsd_verify_attention_fp8_cache), fp32 pages and TSD_ATTN_FORCE_SIMT put the used rows in order in the workspace first.
+ *   workspace    device, 16-byte aligned, tsd_verify_attention_paged_workspace_bytes() bytes (0 for bf16 pages
+ *                without TSD_ATTN_FORCE_SIMT; then NULL is accepted); scratch.
+ * ------------------------------------------------------------------------- */
+size_t tsd_verify_attention_paged_workspace_bytes(const tsd_layout* layout, const tsd_paged_cache* cache, uint32_t flags);
+int tsd_verify_attention_paged(const tsd_layout* layout, const void* mask, const void* q, int64_t q_stride_b,
+                               int64_t q_stride_row, int64_t q_stride_head, const tsd_paged_cache* cache,
+                               const void* k_draft, const void* v_draft, int64_t d_stride_b, int64_t d_stride_row,
+                               int64_t d_stride_head, void* out, int64_t o_stride_b, int64_t o_stride_row,
+                               int64_t o_stride_head, float* lse, float sm_scale, void* workspace,
+                               size_t workspace_bytes, uint32_t flags, uint32_t* status, tsd_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -14,7 +14,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libtsd.so")
 
-TSD_F32, TSD_BF16 = 0, 1
+TSD_F32, TSD_BF16, TSD_E4M3 = 0, 1, 2
 TSD_ACCEPT_EXACT, TSD_ACCEPT_TOP1, TSD_ACCEPT_TOPK, TSD_ACCEPT_PROB = 0, 1, 2, 3
 TSD_SEARCH_GREEDY, TSD_SEARCH_LONGEST = 0, 1
 TSD_ATTN_FORCE_SIMT = 0x1
@@ -32,6 +32,8 @@ EXPORTS = (
     "tsd_commit_accepted", "tsd_verify_attention_fp8_cache_workspace_bytes", "tsd_verify_attention_fp8_cache",
     "tsd_gather_accepted_kv", "tsd_selftest_bounded_wait", "tsd_verify_step",
     "tsd_begin_block", "tsd_advance_block", "tsd_report_block", "tsd_wait_block",
+    "tsd_append_paged_kv", "tsd_paged_attention_workspace_bytes", "tsd_paged_attention",
+    "tsd_verify_attention_paged_workspace_bytes", "tsd_verify_attention_paged",
 )
 
 
@@ -48,6 +50,15 @@ class tsd_layout(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "batch", "n_branches", "rows_per_branch", "n_cache", "n_q_heads", "n_kv_heads",
         "head_dim", "dtype")]
+
+
+class tsd_paged_cache(ctypes.Structure):
+    """Made by make_paged_cache(), which keeps the tensors alive with it."""
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("page_stride", ctypes.c_int64 * 3),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in (
+                    "batch", "n_pages", "page_size", "max_pages", "n_kv_heads", "head_dim", "dtype")]
+    device = -1
 
 
 _lib = None
@@ -103,6 +114,16 @@ def lib():
         L.tsd_verify_attention_fp8_cache.argtypes = (
             [ctypes.POINTER(tsd_layout), _vp] + [_vp, _i64, _i64, _i64] + [_vp, _vp, _i64, _i64, _i64, _vp, _vp]
             + [_vp, _vp, _i64, _i64, _i64] + [_vp, _i64, _i64, _i64] + [_vp, _f32, _vp, _sz, _u32, _vp, _vp])
+        L.tsd_append_paged_kv.argtypes = [_vp, _vp]
+        L.tsd_paged_attention_workspace_bytes.restype = _sz
+        L.tsd_paged_attention_workspace_bytes.argtypes = [ctypes.POINTER(tsd_paged_cache), _i32]
+        L.tsd_paged_attention.argtypes = [ctypes.POINTER(tsd_paged_cache), _i32, _i32, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _f32,
+                                          _vp, _sz, _vp, _vp]
+        L.tsd_verify_attention_paged_workspace_bytes.restype = _sz
+        L.tsd_verify_attention_paged_workspace_bytes.argtypes = [ctypes.POINTER(tsd_layout), ctypes.POINTER(tsd_paged_cache), _u32]
+        L.tsd_verify_attention_paged.argtypes = (
+            [ctypes.POINTER(tsd_layout), _vp] + [_vp, _i64, _i64, _i64] + [ctypes.POINTER(tsd_paged_cache)] + [_vp, _vp, _i64, _i64, _i64]
+            + [_vp, _i64, _i64, _i64] + [_vp, _f32, _vp, _sz, _u32, _vp, _vp])
         _lib = L
     return _lib
 
@@ -119,7 +140,7 @@ def native():
             from . import _tsd_native
         except ImportError as e:
             raise RuntimeError("_tsd_native.so is missing: build it with `python -m paper_2608_27514_b200.build`") from e
-        _tsd_native.setup(torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch.float32, torch.bfloat16, TsdError)
+        _tsd_native.setup(torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch.float32, torch.bfloat16, torch.int32, TsdError)
         _native = _tsd_native
     return _native
 
@@ -331,3 +352,58 @@ def tsd_report_block(n_masked, status, report, ticket, stream=None):
 def tsd_wait_block(report, ticket, stream=None):
     """(largest number of masked rows, status bits) of the pass that reported `ticket`."""
     return native().wait_block(report, ticket, stream)
+
+
+def make_paged_cache(k_pages, v_pages, page_table, k_scale=None, v_scale=None):
+    """Describes a K/V cache in pages: k_pages, v_pages [n_pages, page_size, Hkv, d] (views allowed, same strides, d contiguous) in
+    bf16, fp32 or float8_e4m3fn / uint8 (e4m3 codes); page_table int32 [S, max_pages]; scales fp32 [Hkv], for e4m3 only.  The
+    tensors' contents may change between calls (pages written, table entries set); a reallocated tensor needs a new description."""
+    if not (k_pages.is_cuda and k_pages.device == v_pages.device == page_table.device):
+        raise ValueError("pages and table lie on one CUDA device")
+    if k_pages.dim() != 4 or v_pages.shape != k_pages.shape or v_pages.stride() != k_pages.stride() or v_pages.dtype != k_pages.dtype:
+        raise ValueError("k_pages and v_pages are [n_pages, page_size, heads, head_dim], alike in shape, strides and type")
+    if k_pages.stride(3) != 1:
+        raise ValueError("head_dim must be contiguous")
+    if page_table.dim() != 2 or page_table.dtype != torch.int32 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise ValueError("page_table is int32 [sequences, max_pages], a sequence's entries contiguous")
+    c = tsd_paged_cache()
+    c.n_pages, c.page_size, c.n_kv_heads, c.head_dim = k_pages.shape
+    c.batch, c.max_pages = page_table.shape
+    c.dtype = TSD_E4M3 if k_pages.dtype in (torch.float8_e4m3fn, torch.uint8) else dtype_code(k_pages.dtype)
+    for t in (k_scale, v_scale):
+        if t is not None and (t.dtype != torch.float32 or t.device != k_pages.device or tuple(t.shape) != (c.n_kv_heads,) or not t.is_contiguous()):
+            raise ValueError("scales are contiguous fp32 [heads] beside the pages")
+    c.k_pages, c.v_pages, c.page_table = k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr()
+    c.page_stride[:] = k_pages.stride()[:3]
+    c.table_stride = page_table.stride(0)
+    c.k_scale = None if k_scale is None else k_scale.data_ptr()
+    c.v_scale = None if v_scale is None else v_scale.data_ptr()
+    c.device = k_pages.get_device()
+    c.tensors = (k_pages, v_pages, page_table, k_scale, v_scale)
+    return c
+
+
+def tsd_append_paged_kv(cache, k, v, first_slot=None, n_new=None, positions=None, inv_freq=None, interleaved=False, q=None, q_out=None,
+                        k_out=None, block=None, n_rows=None, status=None, stream=None):
+    """k, v [S, rows, Hkv, d], q [S, rows, Hq, d] (views allowed); first_slot, n_new, block int32 [S]; positions int32 [S, n_rows]; inv_freq
+    fp32 [rotary_dim / 2], None = no rotation.  n_rows: rows of a block, where k holds several (block says which one counts).  cache=None
+    rotates only; q_out and k_out may be q and k."""
+    native().append_paged(cache, k, v, first_slot, n_new, positions, inv_freq, interleaved, q, q_out, k_out, block, n_rows, status, stream)
+
+
+def tsd_paged_attention_workspace_bytes(cache, n_q_heads):
+    return int(lib().tsd_paged_attention_workspace_bytes(ctypes.byref(cache), int(n_q_heads)))
+
+
+def tsd_paged_attention(cache, q, kv_lens, out, lse=None, sm_scale=1.0, workspace=None, status=None, stream=None):
+    """q, out [S, Hq, d]; kv_lens int32 [S] or None (every slot); lse fp32 [S, Hq]; workspace zeroed once."""
+    native().paged_attention(cache, q, kv_lens, out, lse, sm_scale, workspace, status, stream)
+
+
+def tsd_verify_attention_paged_workspace_bytes(layout, cache, flags=0):
+    return int(lib().tsd_verify_attention_paged_workspace_bytes(ctypes.byref(layout), ctypes.byref(cache), int(flags)))
+
+
+def tsd_verify_attention_paged(layout, mask, q, cache, k_draft, v_draft, out, lse=None, sm_scale=1.0, workspace=None, flags=0,
+                               status=None, stream=None):
+    native().verify_attention_paged(layout, mask, q, cache, k_draft, v_draft, out, lse, sm_scale, workspace, flags, status, stream)

@@ -49,6 +49,7 @@
 #include <math_constants.h>
 #include <mutex>
 #include "tsd_common.cuh"
+#include "tsd_paged.cuh"
 
 namespace tsd {
 
@@ -370,7 +371,34 @@ struct TcParams {
   int cut;                        // blocks per item (a cluster), each with a stretch of its key tiles; 1: whole items
   __nv_bfloat16* out;             // where cut items are written without a tensor map
   int64_t os_b, os_r, os_h;
+  const int32_t* table;           // cache in pages of 2^page_shift rows, n_pages of them
+  int64_t table_stride;
+  int page_shift, n_pages;
 };
+
+// A cached tile of 64 keys from its pages: a copy per page that it touches (per 64 rows of a larger one), each with a page as its
+// outermost coordinate.  Rows below `clen` only: behind it a page may not have been handed out, and the copy engine fills what lies outside the pool
+// with zeros.  So it does for an entry that is no page of the pool, which is reported (by the K producer).
+// `page0`: the first entry, asked for before the wait for the stage.
+template <int D>
+__device__ __forceinline__ void load_paged_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int g, int row, int clen, int page0,
+                                                const int32_t* entries, const TcParams& p, bool report) {
+  const int box = min(1 << p.page_shift, kKeys);
+  for (int r = 0; r < kKeys; r += box) {
+    const int key = row + r;
+    int page = -1;
+    if (key < clen) {
+      page = r == 0 ? page0 : entries[key >> p.page_shift];
+      if (page < 0 || page >= p.n_pages) {
+        page = -1;
+        if (report && p.status) atomicOr(p.status, TSD_STATUS_BAD_INDEX);
+      }
+    }
+    const int in_page = key & ((1 << p.page_shift) - 1);
+    tma_load_4d(dst + (uint32_t)r * 128u, map, bar, 0, g, in_page, page);
+    if (D == 128) tma_load_4d(dst + kSubKV + (uint32_t)r * 128u, map, bar, 64, g, in_page, page);
+  }
+}
 
 // The MMAs of a tile go out as ONE block of instructions: the issuing lane shares its scheduler with
 // three softmax warps, so every instruction between two MMAs (a predicate, a 64-bit add for a
@@ -507,7 +535,7 @@ __device__ __noinline__ void copy_q_row(uint32_t q_smem, int r, uint32_t t_q) {
   tmem_wait_st();
 }
 
-template <int D, bool kCut>
+template <int D, bool kCut, bool kPaged>
 __global__ void __launch_bounds__(kTcThreads, 1)
 attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_kc,
                     const __grid_constant__ CUtensorMap map_vc, const __grid_constant__ CUtensorMap map_kd,
@@ -603,6 +631,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                "@c fence.acq_rel.gpu;\n@c fence.proxy.async.global;\n@!c griddepcontrol.wait;\n"
                "@n fence.acq_rel.gpu;\n@n griddepcontrol.launch_dependents;\n}" ::"r"(p.concurrent), "r"(p.next_at_once) : "memory");
   settle(mask);
+  const int32_t* table = p.table;
+  if constexpr (kPaged) settle(table);
 
   const int h_magic = mask[H_MAGIC], h_s = mask[H_S], h_b = mask[H_B], h_r = mask[H_R], h_nc = mask[H_NC];
   // tile counts of this block's items (the blob's layout follows from the tsd_layout, so no
@@ -707,8 +737,14 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         const uint32_t dst = stage0 + t * kKVBytes, full_bar = bar(full0 + t);
         mbar_expect_tx(full_bar, kKVBytes);
         if (is_k && t < kNSb) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], 4;" ::"r"(full_bar) : "memory");
+        if constexpr (kPaged) {
+          const int32_t* entries = table + s_first * p.table_stride;
+          load_paged_tile<D>(dst, mc, full_bar, g_first, (t_first + t) * kKeys, item_clen[0], entries[(t_first + t) * kKeys >> p.page_shift],
+                             entries, p, is_k);
+        } else {
         tma_load_4d(dst, mc, full_bar, 0, g_first, (t_first + t) * kKeys, s_first);
         if (D == 128) tma_load_4d(dst + kSubKV, mc, full_bar, 64, g_first, (t_first + t) * kKeys, s_first);
+        }
       }
       issued = n_pre;
       for (int it = 0; it < n_run && ok; ++it) {
@@ -720,6 +756,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         for (int j = j0; j < j0 + T && ok; ++j, ++G) {
           if (is_k) issue_q(false);
           if (!ok) break;
+          int page0 = 0;
+          if constexpr (kPaged)
+            if (j < n_ct) page0 = table[s * p.table_stride + (j * kKeys >> p.page_shift)];
           // the stage is free once the MMAs that read its previous tile have completed
           if (G >= n_stage) ok = mbar_wait(bar(free0 + b), ph ^ 1u, abort_flag, 100);
           if (!ok) break;
@@ -731,8 +770,12 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
             mbar_expect_tx(full_bar, kKVBytes);
             // no softmax has run before the first three tiles: their S buffers are free from the start
             if (is_k && G < kNSb) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], 4;" ::"r"(full_bar) : "memory");
+            if (kPaged && cached) {
+              load_paged_tile<D>(dst, m, full_bar, g, row, item_clen[it], page0, table + s * p.table_stride, p, is_k);
+            } else {
             tma_load_4d(dst, m, full_bar, 0, g, row, s);
             if (D == 128) tma_load_4d(dst + kSubKV, m, full_bar, 64, g, row, s);
+            }
             issued = G + 1;
           }
           TSD_TR(is_k ? 0 : 1, G);
@@ -1379,27 +1422,28 @@ bool attention_tc_supported(const AttnArgs& a) {
 size_t attention_tc_workspace_bytes(const tsd_layout&) { return 0; }
 
 // The kernels' dynamic shared memory limit, an attribute per device; needed by launches and by questions about them.
-template <int D>
+template <int D, bool kPaged>
 static cudaError_t allow_smem(int dev) {
   static std::mutex mu;
   static bool done[kMaxDevices];
   std::lock_guard<std::mutex> lock(mu);
   if (done[dev]) return cudaSuccess;
-  cudaError_t e = cudaFuncSetAttribute(attention_tc_kernel<D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcSmem<D>::kBytes);
+  cudaError_t e = cudaFuncSetAttribute(attention_tc_kernel<D, false, kPaged>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcSmem<D>::kBytes);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(attention_tc_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcSmem<D>::kBytes);
+    e = cudaFuncSetAttribute(attention_tc_kernel<D, true, kPaged>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcSmem<D>::kBytes);
   done[dev] = e == cudaSuccess;
   return e;
 }
 
 // Blocks per item: a launch with fewer items than SMs leaves SMs idle, so an item's key tiles (T of them, over a full cache) are
-// cut over the 2, 4 or 8 blocks of a cluster, as far as the GPU holds all clusters at one time.
+// cut over the 2, 4 or 8 blocks of a cluster, as far as the GPU holds all clusters at one time (over pages as over a dense cache: the blocks
+// are of one size).
 template <int D>
 static int cut_items(int64_t n_items, int T) {
   static std::mutex mu;
   static int clusters[kMaxDevices][9];  // clusters of that many blocks that run at one time, + 1; 0: not asked yet
   const int dev = current_device();
-  if (dev < 0 || allow_smem<D>(dev) != cudaSuccess) return 1;
+  if (dev < 0 || allow_smem<D, false>(dev) != cudaSuccess) return 1;
   std::lock_guard<std::mutex> lock(mu);
   int best = 1, best_time = T;  // in key tiles
   for (int n = 2, meet = kMeetTiles; n <= (D == 128 ? 8 : 4); n *= 2, meet += 2) {
@@ -1418,7 +1462,7 @@ static int cut_items(int64_t n_items, int T) {
       cfg.attrs = &attr;
       cfg.numAttrs = 1;
       int found = 0;
-      if (cudaOccupancyMaxActiveClusters(&found, attention_tc_kernel<D, true>, &cfg) != cudaSuccess) {
+      if (cudaOccupancyMaxActiveClusters(&found, attention_tc_kernel<D, true, false>, &cfg) != cudaSuccess) {
         cudaGetLastError();
         return best;  // asked again next time
       }
@@ -1446,7 +1490,7 @@ int attention_tc_blocks(const tsd_layout& L) {
   return (int)n_items * (L.head_dim == 64 ? blocks_per_item<64>(L) : blocks_per_item<128>(L));
 }
 
-template <int D>
+template <int D, bool kPaged>
 static int launch_tc(const AttnArgs& a) {
   const tsd_layout& L = a.L;
   const int N = L.n_branches * L.rows_per_branch;
@@ -1455,7 +1499,12 @@ static int launch_tc(const AttnArgs& a) {
             make_map(&mo, a.out, L.batch, N, L.n_q_heads, a.os_b, a.os_r, a.os_h, kTile, D) &&
             make_map(&mkd, a.kd, L.batch, N, L.n_kv_heads, a.ds_b, a.ds_r, a.ds_h, kKeys, D) &&
             make_map(&mvd, a.vd, L.batch, N, L.n_kv_heads, a.ds_b, a.ds_r, a.ds_h, kKeys, D);
-  if (ok && L.n_cache > 0) {
+  if (ok && kPaged) {  // pages for sequences, their rows for rows
+    const PagedView& c = *a.pages;
+    const int rows = 1 << c.shift, box = std::min(rows, kKeys);
+    ok = make_map(&mkc, c.k, c.n_pages, rows, L.n_kv_heads, c.ps_p, c.ps_r, c.ps_h, box, D) &&
+         make_map(&mvc, c.v, c.n_pages, rows, L.n_kv_heads, c.ps_p, c.ps_r, c.ps_h, box, D);
+  } else if (ok && L.n_cache > 0) {
     ok = make_map(&mkc, a.kc, L.batch, L.n_cache, L.n_kv_heads, a.cs_b, a.cs_r, a.cs_h, kKeys, D) &&
          make_map(&mvc, a.vc, L.batch, L.n_cache, L.n_kv_heads, a.cs_b, a.cs_r, a.cs_h, kKeys, D);
   } else if (ok) {  // no cache: the cached maps are never dereferenced
@@ -1464,10 +1513,11 @@ static int launch_tc(const AttnArgs& a) {
   }
   const MaskDims md = mask_dims(L);
   const int64_t n_items = (int64_t)L.batch * L.n_q_heads * md.n_qt;
-  if (!ok || n_items > 0x7fffffffLL / 4 || md.bytes / 4 > 0xffffffffu) return launch_attention_simt(a);  // strides the tensor maps cannot express
+  if (!ok || n_items > 0x7fffffffLL / 4 || md.bytes / 4 > 0xffffffffu)  // strides the tensor maps cannot express
+    return kPaged ? TSD_ERR_UNSUPPORTED : launch_attention_simt(a);
   const int dev = current_device();
   if (dev < 0) return cuda_fail(cudaErrorInvalidDevice, "cudaGetDevice");
-  const cudaError_t attr_err = allow_smem<D>(dev);
+  const cudaError_t attr_err = allow_smem<D, kPaged>(dev);
   if (attr_err != cudaSuccess) return cuda_fail(attr_err, "cudaFuncSetAttribute(attention_tc_kernel)");
   TcParams p;
   p.mask = a.mask;
@@ -1486,8 +1536,12 @@ static int launch_tc(const AttnArgs& a) {
   p.cut = blocks_per_item<D>(L);
   p.out = static_cast<__nv_bfloat16*>(a.out);
   p.os_b = a.os_b; p.os_r = a.os_r; p.os_h = a.os_h;
+  p.table = kPaged ? a.pages->table : nullptr;
+  p.table_stride = kPaged ? a.pages->table_stride : 0;
+  p.page_shift = kPaged ? a.pages->shift : 0;
+  p.n_pages = kPaged ? a.pages->n_pages : 0;
   if (p.cut > 1) {
-    cudaError_t e = launch_clusters(p.cut, attention_tc_kernel<D, true>, (unsigned)(n_items * p.cut), kTcThreads, TcSmem<D>::kBytes, a.stream,
+    cudaError_t e = launch_clusters(p.cut, attention_tc_kernel<D, true, kPaged>, (unsigned)(n_items * p.cut), kTcThreads, TcSmem<D>::kBytes, a.stream,
                                     mq, mkc, mvc, mkd, mvd, mo, p);
     return e != cudaSuccess ? cuda_fail(e, "attention_tc_kernel") : TSD_OK;
   }
@@ -1496,13 +1550,16 @@ static int launch_tc(const AttnArgs& a) {
   // items of 8 tiles on 148 SMs: 1.56 and 2.71-2.83 ms; in whole rounds 1.56 and 1.59).
   const int64_t sms = std::max(device_facts().sms, 1);
   const int64_t grid = std::min(n_items, sms * ((n_items + sms * kMaxItems - 1) / (sms * kMaxItems)));
-  cudaError_t e = launch(attention_tc_kernel<D, false>, (unsigned)grid, kTcThreads, TcSmem<D>::kBytes, a.stream, mq, mkc, mvc, mkd,
+  cudaError_t e = launch(attention_tc_kernel<D, false, kPaged>, (unsigned)grid, kTcThreads, TcSmem<D>::kBytes, a.stream, mq, mkc, mvc, mkd,
                          mvd, mo, p);
   if (e != cudaSuccess) return cuda_fail(e, "attention_tc_kernel");
   return TSD_OK;
 }
 
-int launch_attention_tc(const AttnArgs& a) { return a.L.head_dim == 64 ? launch_tc<64>(a) : launch_tc<128>(a); }
+int launch_attention_tc(const AttnArgs& a) {
+  if (a.pages) return a.L.head_dim == 64 ? launch_tc<64, true>(a) : launch_tc<128, true>(a);
+  return a.L.head_dim == 64 ? launch_tc<64, false>(a) : launch_tc<128, false>(a);
+}
 
 }  // namespace tsd
 

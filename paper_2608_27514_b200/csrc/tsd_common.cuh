@@ -56,6 +56,7 @@ int check_attention_args(const tsd_layout* L, const void* mask, const void* q, i
                          float sm_scale, const void* workspace);
 
 // attention launchers (defined in their own translation units)
+struct PagedView;
 struct AttnArgs {
   tsd_layout L;
   const int32_t* mask;
@@ -70,6 +71,7 @@ struct AttnArgs {
   cudaStream_t stream;
   bool concurrent;    // reads nothing that the kernel before it in the stream writes: may run beside it
   bool next_at_once;  // the next kernel may be brought up once all blocks of this one run
+  const PagedView* pages = nullptr;  // the cache in pages (kc, vc unused); the tensor-core kernel only
 };
 int launch_attention_simt(const AttnArgs& a);
 bool attention_tc_supported(const AttnArgs& a);

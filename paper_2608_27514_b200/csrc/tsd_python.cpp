@@ -9,8 +9,8 @@
 
 namespace {
 
-PyObject *n_data_ptr, *n_stride, *n_shape, *n_nbytes, *n_dtype, *n_cuda_stream, *n_is_contiguous;
-PyObject *get_device, *get_raw_stream, *dtype_f32, *dtype_bf16, *error_type;  // set by setup()
+PyObject *n_data_ptr, *n_stride, *n_shape, *n_nbytes, *n_dtype, *n_cuda_stream, *n_is_contiguous, *n_get_device, *n_device;
+PyObject *get_device, *get_raw_stream, *dtype_f32, *dtype_bf16, *dtype_i32, *error_type;  // set by setup()
 
 struct Failed {};  // a Python exception is set
 
@@ -111,18 +111,22 @@ tsd_stream_t stream_of(PyObject* s) {
   PyErr_Clear();
   return reinterpret_cast<tsd_stream_t>((uintptr_t)to_int(s));
 }
-struct Layout {  // a ctypes structure, read through the buffer protocol
+template <typename T>
+struct Structure {  // a ctypes structure, read through the buffer protocol
   Py_buffer b;
-  explicit Layout(PyObject* o) {
+  Structure(PyObject* o, const char* wanted) {
     if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE)) throw Failed{};
-    if (b.len != (Py_ssize_t)sizeof(tsd_layout)) {
+    if (b.len != (Py_ssize_t)sizeof(T)) {
       PyBuffer_Release(&b);
-      PyErr_SetString(PyExc_TypeError, "a tsd_layout is wanted");
+      PyErr_SetString(PyExc_TypeError, wanted);
       throw Failed{};
     }
   }
-  ~Layout() { PyBuffer_Release(&b); }
-  const tsd_layout* get() const { return static_cast<const tsd_layout*>(b.buf); }
+  ~Structure() { PyBuffer_Release(&b); }
+  const T* get() const { return static_cast<const T*>(b.buf); }
+};
+struct Layout : Structure<tsd_layout> {
+  explicit Layout(PyObject* o) : Structure(o, "a tsd_layout is wanted") {}
 };
 // the call itself runs without the interpreter lock
 template <typename... P, typename... A>
@@ -140,8 +144,8 @@ PyObject* done(int rc, const char* where) {
 using Args = PyObject* const*;
 
 PyObject* setup(Args a) {
-  PyObject** to[] = {&get_device, &get_raw_stream, &dtype_f32, &dtype_bf16, &error_type};
-  for (int i = 0; i < 5; ++i) {
+  PyObject** to[] = {&get_device, &get_raw_stream, &dtype_f32, &dtype_bf16, &dtype_i32, &error_type};
+  for (int i = 0; i < 6; ++i) {
     Py_INCREF(a[i]);
     Py_XSETREF(*to[i], a[i]);
   }
@@ -394,6 +398,165 @@ PyObject* advance_block(Args a) {
   return done(call(tsd_advance_block, &t, stream_of(a[36])), "tsd_advance_block");
 }
 
+// ---- the calls on a paged cache check what they are given: sizes, types, and that it lies on the current device
+struct Here {
+  int64_t device;
+  Here() {
+    Ref d(PyObject_CallNoArgs(get_device));
+    device = to_int(d.p);
+  }
+  void operator()(PyObject* t) const {  // None is fine
+    if (t == Py_None) return;
+    Ref d(PyObject_CallMethodNoArgs(t, n_get_device));
+    want(to_int(d.p) == device, "tensors lie on the current CUDA device");
+  }
+};
+struct Pages : Structure<tsd_paged_cache> {
+  Pages(PyObject* o, const Here& here) : Structure(o, "a tsd_paged_cache is wanted") {
+    Ref d(PyObject_GetAttr(o, n_device));
+    want(to_int(d.p) == here.device, "the cache lies on the current CUDA device");
+  }
+};
+void typed(PyObject* t, PyObject* dtype, const char* what) {
+  Ref d(PyObject_GetAttr(t, n_dtype));
+  want(d.p == dtype, what);
+}
+// contiguous int32 (fp32) of `count` elements, or None
+template <typename T>
+T* vec(PyObject* t, PyObject* dtype, int64_t count, const Here& here, const char* what) {
+  if (t == Py_None) return nullptr;
+  here(t);
+  typed(t, dtype, what);
+  want(contiguous(t) && (int64_t)nbytes(t) == count * 4, what);
+  return ptr<T>(t);
+}
+struct Rows {  // [batch, rows, heads, dim], dim contiguous
+  int64_t n[4], st[4];
+  Rows(PyObject* t, const Here& here) {
+    here(t);
+    want(shape(t, n) == 4, "[sequences, rows, heads, head_dim] is wanted");
+    want(strides(t, st) == 4 && (n[3] == 1 || st[3] == 1), "head_dim must be contiguous");
+  }
+  void as(PyObject* t, const Rows& o, bool heads_too, PyObject* u) const {  // `t`, these rows, has the type and the sizes of `u`
+    Ref a(PyObject_GetAttr(t, n_dtype)), b(PyObject_GetAttr(u, n_dtype));
+    want(a.p == b.p, "types differ");
+    want(n[0] == o.n[0] && n[1] == o.n[1] && (!heads_too || n[2] == o.n[2]) && n[3] == o.n[3], "shapes differ");
+  }
+  void along(const Rows& o) const {  // one set of strides serves both (where a dimension has one entry, any stride does)
+    for (int i = 0; i < 3; ++i) want(n[i] <= 1 || st[i] == o.st[i], "K and V strides differ");
+  }
+  void to(int64_t (&out)[3]) const {
+    for (int i = 0; i < 3; ++i) out[i] = st[i];
+  }
+};
+int32_t small(int64_t v) {
+  want(v >= 0 && v <= 0x7fffffff, "a size is too large");
+  return (int32_t)v;
+}
+
+// cache (or None), k, v, first_slot, n_new, positions, inv_freq, interleaved, q, q_out, k_out, block, n_rows, status, stream
+PyObject* append_paged(Args a) {
+  const Here here;
+  tsd_append_args t = {};
+  const Rows k(a[1], here);
+  t.dtype = dtype_code(a[1]);
+  k.to(t.kv_stride);
+  t.batch = small(k.n[0]);
+  t.n_rows = a[12] == Py_None ? small(k.n[1]) : to_i32(a[12]);
+  want(t.n_rows >= 0 && (t.n_rows == 0 ? k.n[1] == 0 : k.n[1] % t.n_rows == 0), "the rows are whole blocks of n_rows");
+  t.n_blocks = t.n_rows ? small(k.n[1] / t.n_rows) : 1;
+  if (t.n_blocks == 0) { t.n_blocks = 1; t.n_rows = 0; }
+  t.n_kv_heads = small(k.n[2]);
+  t.head_dim = small(k.n[3]);
+  t.k = ptr(a[1]);
+  if (a[2] != Py_None) {
+    const Rows v(a[2], here);
+    v.as(a[2], k, true, a[1]);
+    v.along(k);
+    t.v = ptr(a[2]);
+  }
+  if (a[8] != Py_None) {
+    want(a[9] != Py_None, "q wants a q_out");
+    const Rows q(a[8], here), o(a[9], here);
+    q.as(a[8], k, false, a[1]);
+    o.as(a[9], q, true, a[8]);
+    t.n_q_heads = small(q.n[2]);
+    q.to(t.q_stride);
+    o.to(t.q_out_stride);
+    t.q = ptr(a[8]);
+    t.q_out = ptr(a[9]);
+  } else {
+    want(a[9] == Py_None, "q_out wants a q");
+  }
+  if (a[10] != Py_None) {
+    const Rows o(a[10], here);
+    o.as(a[10], k, true, a[1]);
+    o.to(t.k_out_stride);
+    t.k_out = ptr(a[10]);
+  }
+  t.first_slot = vec<int32_t>(a[3], dtype_i32, t.batch, here, "first_slot is a contiguous int32 [sequences]");
+  t.n_new = vec<int32_t>(a[4], dtype_i32, t.batch, here, "n_new is a contiguous int32 [sequences]");
+  t.positions = vec<int32_t>(a[5], dtype_i32, (int64_t)t.batch * t.n_rows, here, "positions is a contiguous int32 [sequences, n_rows]");
+  t.block = vec<int32_t>(a[11], dtype_i32, t.batch, here, "block is a contiguous int32 [sequences]");
+  if (a[6] != Py_None) {
+    t.rotary_dim = small((int64_t)nbytes(a[6]) / 2);  // 4 bytes for every two dimensions
+    t.inv_freq = vec<float>(a[6], dtype_f32, t.rotary_dim / 2, here, "inv_freq is a contiguous fp32 [rotary_dim / 2]");
+  }
+  t.interleaved = PyObject_IsTrue(a[7]);
+  here(a[13]);
+  t.status = ptr<uint32_t>(a[13]);
+  if (a[0] == Py_None) return done(call(tsd_append_paged_kv, &t, stream_of(a[14])), "tsd_append_paged_kv");
+  const Pages cache(a[0], here);
+  t.cache = cache.get();
+  return done(call(tsd_append_paged_kv, &t, stream_of(a[14])), "tsd_append_paged_kv");
+}
+
+// cache, q, kv_lens, out, lse, sm_scale, workspace, status, stream
+PyObject* paged_attention(Args a) {
+  const Here here;
+  const Pages cache(a[0], here);
+  int64_t q[4], o[4], qs[4], os[4];
+  here(a[1]);
+  here(a[3]);
+  want(shape(a[1], q) == 3 && shape(a[3], o) == 3 && q[0] == o[0] && q[1] == o[1] && q[2] == o[2], "q and out are [sequences, heads, head_dim]");
+  want(strides(a[1], qs) == 3 && strides(a[3], os) == 3 && qs[2] == 1 && os[2] == 1, "head_dim must be contiguous");
+  want(q[0] == cache.get()->batch && q[2] == cache.get()->head_dim, "q has the cache's sequences and head_dim");
+  const int32_t dtype = dtype_code(a[1]);
+  want(dtype_code(a[3]) == dtype, "types of q and out differ");
+  here(a[6]);
+  here(a[7]);
+  return done(call(tsd_paged_attention, cache.get(), small(q[1]), dtype, ptr(a[1]), qs[0], qs[1],
+                   vec<int32_t>(a[2], dtype_i32, q[0], here, "kv_lens is a contiguous int32 [sequences]"), ptr(a[3]), os[0], os[1],
+                   vec<float>(a[4], dtype_f32, q[0] * q[1], here, "lse is a contiguous fp32 [sequences, heads]"), to_float(a[5]), ptr(a[6]),
+                   nbytes(a[6]), ptr<uint32_t>(a[7]), stream_of(a[8])),
+              "tsd_paged_attention");
+}
+
+// layout, mask, q, cache, k_draft, v_draft, out, lse, sm_scale, workspace, flags, status, stream
+PyObject* verify_attention_paged(Args a) {
+  const Here here;
+  Layout L(a[0]);
+  const tsd_layout* l = L.get();
+  const Pages cache(a[3], here);
+  const Rows q(a[2], here), k(a[4], here), v(a[5], here), o(a[6], here);
+  want(q.n[0] == l->batch && q.n[1] == (int64_t)l->n_branches * l->rows_per_branch && q.n[2] == l->n_q_heads && q.n[3] == l->head_dim,
+       "q is [batch, branches * rows, n_q_heads, head_dim] of the layout");
+  k.as(a[4], q, false, a[2]);
+  want(k.n[2] == l->n_kv_heads && dtype_code(a[2]) == l->dtype, "draft rows have the layout's heads and type");
+  v.as(a[5], k, true, a[4]);
+  v.along(k);
+  o.as(a[6], q, true, a[2]);
+  here(a[1]);
+  here(a[9]);
+  here(a[11]);
+  want(a[1] != Py_None && nbytes(a[1]) >= tsd_branch_mask_bytes(l), "the mask is that of the layout");
+  return done(call(tsd_verify_attention_paged, l, ptr(a[1]), ptr(a[2]), q.st[0], q.st[1], q.st[2], cache.get(), ptr(a[4]), ptr(a[5]),
+                   k.st[0], k.st[1], k.st[2], ptr(a[6]), o.st[0], o.st[1], o.st[2],
+                   vec<float>(a[7], dtype_f32, q.n[0] * q.n[1] * q.n[2], here, "lse is a contiguous fp32 [batch, heads, rows]"),
+                   to_float(a[8]), ptr(a[9]), nbytes(a[9]), (uint32_t)to_int(a[10]), ptr<uint32_t>(a[11]), stream_of(a[12])),
+              "tsd_verify_attention_paged");
+}
+
 // n_masked [S], status, report, ticket, stream
 PyObject* report_block(Args a) {
   int64_t s[4];
@@ -429,12 +592,13 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 #define TSD_METHOD(f, n) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<f, n>)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {TSD_METHOD(setup, 5),           TSD_METHOD(verify_attention, 14), TSD_METHOD(verify_attention_fp8, 16),
+PyMethodDef methods[] = {TSD_METHOD(setup, 6),           TSD_METHOD(verify_attention, 14), TSD_METHOD(verify_attention_fp8, 16),
                          TSD_METHOD(confidence_topk, 9), TSD_METHOD(accept, 19),           TSD_METHOD(accept_relaxed, 22),
                          TSD_METHOD(commit, 15),         TSD_METHOD(build_tree, 18),       TSD_METHOD(build_mask, 6),
                          TSD_METHOD(verify_step, 34),    TSD_METHOD(interblock_vis, 3),    TSD_METHOD(interblock_trigger, 10),
                          TSD_METHOD(begin_block, 13),    TSD_METHOD(advance_block, 38),    TSD_METHOD(report_block, 5),
-                         TSD_METHOD(wait_block, 3),
+                         TSD_METHOD(wait_block, 3),      TSD_METHOD(append_paged, 15),     TSD_METHOD(paged_attention, 9),
+                         TSD_METHOD(verify_attention_paged, 13),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tsd_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -448,5 +612,7 @@ PyMODINIT_FUNC PyInit__tsd_native(void) {
   n_dtype = PyUnicode_InternFromString("dtype");
   n_cuda_stream = PyUnicode_InternFromString("cuda_stream");
   n_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+  n_get_device = PyUnicode_InternFromString("get_device");
+  n_device = PyUnicode_InternFromString("device");
   return PyModule_Create(&module);
 }

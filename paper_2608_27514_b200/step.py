@@ -40,6 +40,7 @@ class VerifyStep:
         self.unmask_flag = torch.empty((S, R), dtype=torch.uint8, device=dev)
         self.unmask_tok = torch.empty((S, R), dtype=torch.int32, device=dev)
         self.status = torch.zeros(1, dtype=torch.int32, device=dev)
+        self.paged_ws = None  # of attention_paged(), from the first call that asks for one
         self.mask_built = False
 
     @classmethod
@@ -58,6 +59,20 @@ class VerifyStep:
                                self.attn_lse if lse is None else lse, sm_scale, self.attn_ws, flags,
                                self.status)
         return self.out if out is None else out
+
+    def attention_paged(self, q, cache, k_draft, v_draft, sm_scale, flags=0, out=None, lse=None):
+        """attention() with the cached keys and values in pages (binding.make_paged_cache())."""
+        if not self.mask_built:
+            self.build_mask()
+        need = B.tsd_verify_attention_paged_workspace_bytes(self.layout, cache, flags)
+        if need > 0 and self.paged_ws is None:  # as large for every cache of this layout
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("the first call on 8-bit or fp32 pages allocates a workspace: make one before the capture")
+            self.paged_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        out = self.out if out is None else out
+        B.tsd_verify_attention_paged(self.layout, self.mask, q, cache, k_draft, v_draft, out, self.attn_lse if lse is None else lse,
+                                     sm_scale, self.paged_ws, flags, self.status)
+        return out
 
     def confidence_topk(self, logits):
         B.tsd_confidence_topk(logits, self.k, self.conf, self.topk_idx, self.topk_prob, self.lse,

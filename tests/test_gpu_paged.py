@@ -1,0 +1,589 @@
+"""The paged K/V cache on the GPU: new rows against the oracle, one token's attention against the oracle, a verification pass over pages bit for
+bit against the same pass over a dense cache, and the calls together.
+
+Tolerances, with u = 2^-24: a rotated value is the rounding (half a step of its type) of two fp32 products with a cosine and a sine that
+are off by at most 1.2e-7 (an angle of at most an eighth of a turn rounded to fp32, 4.7e-8, and 1 ulp of the functions): 3e-7 (|x| + |y|).  A
+score of d products summed in fp32 is off by at most d u sum |q_i k_i| and its exponent by 2 u |s| more (scale, subtraction); a weight is
+then off by that, relatively, and by 2^-16 (two bf16 parts; 2^-22 in fp32), an output by twice that times max |v|, and by half a step of its type."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged as oracle
+from paper_2608_27514_b200 import binding as B
+from paper_2608_27514_b200.step import VerifyStep
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+FP8 = torch.float8_e4m3fn
+TYPES = {"bf16": (torch.bfloat16, torch.bfloat16), "f32": (torch.float32, torch.float32), "e4m3": (torch.bfloat16, FP8)}
+HALF_STEP = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24, FP8: 2.0 ** -4}
+
+
+def _np(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+def _rnd(gen, *shape, dtype=torch.float32):
+    return torch.randn(shape, generator=gen, device=DEV).to(dtype)
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+class Pool:
+    """Pages of random values, handed out in random order; heads and rows may be strided."""
+
+    def __init__(self, kind, tokens, Hkv, d, page, seed=0, spare=3, head_major=False, fill=None):
+        self.kind, self.page, self.dtype = kind, page, TYPES[kind][0]
+        gen = torch.Generator(device=DEV).manual_seed(seed)
+        need = [-(-t // page) for t in tokens]
+        n_pages, per = sum(need) + spare, max(1, max(need))
+        order = torch.randperm(n_pages, generator=gen, device=DEV)
+        table = torch.full((len(tokens), per), -1, dtype=torch.int32)
+        at = 0
+        for s, n in enumerate(need):
+            table[s, :n] = order[at:at + n].cpu().to(torch.int32)
+            at += n
+        self.table = table.to(DEV)
+        shape = (n_pages, Hkv, page, d) if head_major else (n_pages, page, Hkv, d)
+        self.scale = {}
+        self.pages = {}
+        for name in "kv":
+            x = _rnd(gen, *shape)
+            x = x.transpose(1, 2) if head_major else x
+            if kind == "e4m3":
+                self.scale[name] = (0.5 + torch.rand(Hkv, generator=gen, device=DEV)) / 64
+                x = (x / self.scale[name][:, None]).clamp(-448, 448).to(FP8)
+            else:
+                self.scale[name] = None
+                x = x.to(TYPES[kind][1])
+            self.pages[name] = x
+        if fill is not None:  # what nobody may use: rows at or past `fill[s]`, and the spare pages
+            live = torch.zeros((n_pages, page), dtype=torch.bool)
+            for s, n in enumerate(fill):
+                for t in range(min(n, tokens[s])):
+                    live[int(table[s, t // page]), t % page] = True
+            dead = ~live.to(DEV)
+            for x in self.pages.values():
+                if kind == "e4m3":
+                    x.view(torch.uint8)[dead] = 0x7F
+                else:
+                    x[dead] = float("nan")
+        self.cache = B.make_paged_cache(self.pages["k"], self.pages["v"], self.table, self.scale["k"], self.scale["v"])
+
+    def codes(self, name):
+        x = self.pages[name]
+        return (x.view(torch.uint8) if self.kind == "e4m3" else x).clone()
+
+    def dense(self, name, s, length):
+        """fp64 values of one sequence."""
+        x = oracle.ordered(_np(self.pages[name]), self.table[s].cpu().numpy(), length)
+        return x if self.scale[name] is None else x * _np(self.scale[name])[None, :, None]
+
+
+# ------------------------------------------------------------------------------------------ append
+def _check_rotated(got, ref, size, dtype):
+    tol = HALF_STEP[dtype] * (np.abs(ref) + 3e-7 * size) + 3e-7 * size + (2.0 ** -10 if dtype == FP8 else 1e-38)
+    assert (np.abs(got - ref) <= tol).all(), np.abs(got - ref).max()
+
+
+def _pair_size(x, half, interleaved):
+    """|x| + |y| over the pair of every dimension."""
+    a = np.abs(np.array(x, dtype=np.float64))
+    if half and interleaved:
+        s = a[..., 0:2 * half:2] + a[..., 1:2 * half:2]
+        a[..., 0:2 * half:2], a[..., 1:2 * half:2] = s, s
+    elif half:
+        s = a[..., :half] + a[..., half:2 * half]
+        a[..., :half], a[..., half:2 * half] = s, s
+    return a
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("kind", ["bf16", "f32", "e4m3"])
+@pytest.mark.parametrize("S,n,Hq,Hkv,d,page,rot,start,ragged", [
+    (1, 1, 32, 32, 128, 64, 128, [0], False), (3, 1, 28, 4, 128, 16, 128, [5, 77, 15], False), (2, 37, 4, 4, 64, 8, 64, [3, 100], True),
+    (4, 70, 8, 1, 128, 32, 32, [0, 31, 32, 33], True), (2, 5, 3, 3, 64, 1024, 16, [1020, 1023], False), (2, 20, 2, 2, 128, 128, 0, [9, 127], True)])
+def test_append(kind, interleaved, S, n, Hq, Hkv, d, page, rot, start, ragged):
+    gen = torch.Generator(device=DEV).manual_seed(n + d)
+    dt, ct = TYPES[kind]
+    pool = Pool(kind, [a + n for a in start], Hkv, d, page, seed=3, head_major=page == 32)
+    k, v, q = _rnd(gen, S, n, Hkv, d, dtype=dt), _rnd(gen, S, n, Hkv, d, dtype=dt), _rnd(gen, S, n, Hq, d, dtype=dt)
+    n_new = [n, 0, 1, n + 5][:S] if ragged else None
+    freq = (1e4 ** (-torch.arange(0, rot, 2, device=DEV) / max(rot, 1))).float() if rot else None
+    before = {x: pool.codes(x) for x in "kv"}
+    q_out, k_out = torch.full_like(q, 7.0), torch.full_like(k, 7.0)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.tsd_append_paged_kv(pool.cache, k, v, _i32(start), None if n_new is None else _i32(n_new), inv_freq=freq, interleaved=interleaved, q=q,
+                          q_out=q_out, k_out=k_out, status=status)
+    torch.cuda.synchronize()
+    assert status.item() == 0
+    f = [] if freq is None else _np(freq)
+    touched = torch.zeros(pool.pages["k"].shape[:2], dtype=torch.bool, device=DEV)
+    for s in range(S):
+        m = n if n_new is None else min(n_new[s], n)
+        pos = start[s] + np.arange(m)
+        at = oracle.slots(start[s], m, pool.table[s].cpu().numpy(), page, pool.cache.n_pages)
+        pages, rows = [torch.tensor([a[i] for a in at], dtype=torch.long, device=DEV) for i in (0, 1)]
+        touched[pages, rows] = True
+        for x, name in ((k, "k"), (v, "v")):
+            here = _np(x[s, :m])
+            ref = oracle.rotate(here, pos, f if name == "k" else [], interleaved)
+            size = _pair_size(here, len(f) if name == "k" else 0, interleaved)
+            if name == "k":
+                _check_rotated(_np(k_out[s, :m]), ref, size, dt)
+            if kind == "e4m3":
+                sc = _np(pool.scale[name])[None, :, None]
+                ref, size = np.clip(ref / sc, -448, 448), size / sc
+            got = _np(pool.pages[name].view(torch.uint8)[pages, rows].view(FP8) if kind == "e4m3" else pool.pages[name][pages, rows])
+            _check_rotated(got, ref, size, ct)
+            if name == "v" and kind != "e4m3":
+                assert np.array_equal(got, here)
+        here = _np(q[s, :m])
+        _check_rotated(_np(q_out[s, :m]), oracle.rotate(here, pos, f, interleaved), _pair_size(here, len(f), interleaved), dt)
+        assert bool((q_out[s, m:] == 7).all()) and bool((k_out[s, m:] == 7).all())       # rows that do not count stay
+    for x in "kv":                                                                       # and so do all other slots
+        assert torch.equal(pool.codes(x)[~touched], before[x][~touched])
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_far_and_negative_positions(interleaved):
+    # positions whose angle fp32 does not hold, and a frequency that makes the angle pass 2^32 quarters
+    pos = [[1 << 20, 999983, 131071], [0x7fffffff, -1, -131071]]
+    freq = torch.tensor([1.0, 0.7310586, 1e-4, 12345.678, 0.0, 3.1415927, 1e-30, 0.25], device=DEV)
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    k = _rnd(gen, 2, 3, 2, 64)
+    out = torch.empty_like(k)
+    B.tsd_append_paged_kv(None, k, None, positions=_i32(pos), inv_freq=freq, interleaved=interleaved, k_out=out)
+    ref = oracle.rotate(_np(k), np.array(pos), _np(freq), interleaved)
+    # numpy's own angle is rounded to 53 bits: 2^31 x 12345 x 2^-53 = 3e-3 at the far end, so it is reduced exactly here
+    from fractions import Fraction
+    import math
+    two_pi = Fraction(2 * math.pi) + Fraction(2.4492935982947064e-16)                  # 2 pi to 106 bits
+    exact = np.zeros((2, 3, 8))
+    for s in range(2):
+        for i in range(3):
+            for j in range(8):
+                a = Fraction(pos[s][i]) * Fraction(float(freq[j]))
+                exact[s, i, j] = float(a - two_pi * round(a / two_pi))
+    z = np.exp(1j * exact)[:, :, None]
+    x = _np(k)
+    re, im = (x[..., 0:16:2], x[..., 1:16:2]) if interleaved else (x[..., :8], x[..., 8:16])
+    w = (re + 1j * im) * z
+    ref = x.copy()
+    if interleaved:
+        ref[..., 0:16:2], ref[..., 1:16:2] = w.real, w.imag
+    else:
+        ref[..., :8], ref[..., 8:16] = w.real, w.imag
+    # the kernel's angle in turns is rounded to 53 bits twice: 2^-52 of it, in radians 2^-52 x |angle|
+    far = np.abs(np.array(pos))[..., None] * np.abs(_np(freq)) * 2.0 ** -52 * 2
+    far = np.concatenate([far, far], -1)[..., None, :] if not interleaved else np.repeat(far, 2, -1)[..., None, :]
+    size = _pair_size(x, 8, interleaved)
+    tol = 2.0 ** -24 * np.abs(ref) + 3e-7 * size
+    tol[..., :16] += far * size[..., :16]
+    assert (np.abs(_np(out) - ref) <= tol).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_the_accepted_block_goes_to_its_pages(kind):
+    # the rows of one node of many, unrotated, the same bytes that the hand-over into a dense cache gives; views with other strides
+    S, Bn, R, H, d, page = 3, 7, 32, 4, 64, 16
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    both = _rnd(gen, S, Bn * R, 2 * H, d, dtype=TYPES[kind][0])
+    k, v = both[:, :, :H], both[:, :, H:]
+    node, start = _i32([6, 0, 3]), [40, 0, 17]
+    pool = Pool(kind, [a + R for a in start], H, d, page)
+    B.tsd_append_paged_kv(pool.cache, k, v, _i32(start), block=node, n_rows=R)
+    dense = [torch.zeros((S, 80, H, d), dtype=k.dtype, device=DEV) for _ in range(2)]
+    B.tsd_gather_accepted_kv(node, R, k, v, dense[0], dense[1], _i32(start))
+    for s in range(S):
+        for i, name in enumerate("kv"):
+            assert np.array_equal(pool.dense(name, s, start[s] + R)[start[s]:], _np(dense[i][s, start[s]:start[s] + R]))
+
+
+def test_rotation_in_place_and_alone():
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    q, k = _rnd(gen, 2, 9, 4, 128, dtype=torch.bfloat16), _rnd(gen, 2, 9, 2, 128, dtype=torch.bfloat16)
+    freq = torch.rand(32, generator=gen, device=DEV)
+    pos = torch.randint(0, 5000, (2, 9), generator=gen, device=DEV, dtype=torch.int32)
+    q_out, k_out = torch.empty_like(q), torch.empty_like(k)
+    B.tsd_append_paged_kv(None, k, None, positions=pos, inv_freq=freq, q=q, q_out=q_out, k_out=k_out)
+    B.tsd_append_paged_kv(None, k, None, positions=pos, inv_freq=freq, q=q, q_out=q, k_out=k)
+    assert torch.equal(q, q_out) and torch.equal(k, k_out) and not torch.equal(q[:, :, :, :64], q[:, :, :, 64:])
+
+
+def test_slots_that_do_not_exist():
+    # a page outside the pool, one not handed out, slots in front of and behind the table, a block that is none: reported, not written
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    pool = Pool("bf16", [40, 40, 40, 40], 2, 64, 8)
+    pool.table[1, 3], pool.table[1, 4] = -1, 1 << 30
+    k, v, q = [_rnd(gen, 4, 2 * 6, h, 64, dtype=torch.bfloat16) for h in (2, 2, 4)]
+    q_out = torch.zeros_like(q)
+    start, block = [36, 22, -3, 0], [1, 0, 0, 2]
+    before = {x: pool.codes(x) for x in "kv"}
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.tsd_append_paged_kv(pool.cache, k, v, _i32(start), q=q, q_out=q_out, block=_i32(block), n_rows=6, status=status)
+    assert B.tsd_check_status(status) == B.TSD_ERR_DEVICE_DATA
+    changed = torch.zeros(pool.pages["k"].shape[:2], dtype=torch.bool, device=DEV)
+    for s in range(3):
+        for i, (p, r) in enumerate(oracle.slots(start[s], 6, pool.table[s].cpu().numpy(), 8, pool.cache.n_pages)):
+            if p >= 0:
+                changed[p, r] = True
+                assert torch.equal(pool.pages["k"][p, r], k[s, block[s] * 6 + i]) and torch.equal(pool.pages["v"][p, r], v[s, block[s] * 6 + i])
+        assert torch.equal(q_out[s, block[s] * 6:block[s] * 6 + 6], q[s, block[s] * 6:block[s] * 6 + 6])
+    assert int(changed.sum()) == 4 + 2 + 3                                              # slots 36-39; 22, 23; 0-2
+    assert not q_out[3].any()
+    for x in "kv":
+        assert torch.equal(pool.codes(x)[~changed], before[x][~changed])
+    # a zero scale, infinities and values beyond 448 scales saturate
+    pool = Pool("e4m3", [8], 2, 64, 8)
+    x = torch.full((1, 1, 2, 64), float("inf"), dtype=torch.bfloat16, device=DEV)
+    B.tsd_append_paged_kv(pool.cache, x, -x)
+    assert bool((pool.pages["k"].view(torch.uint8)[int(pool.table[0, 0]), 0] == 0x7E).all())
+    assert bool((pool.pages["v"].view(torch.uint8)[int(pool.table[0, 0]), 0] == 0xFE).all())
+
+
+# ------------------------------------------------------------------------------------------- token
+def _token(pool, q, lens, sm_scale, workspace=None, out=None, stream=None):
+    S, Hq, d = q.shape
+    if workspace is None:
+        workspace = torch.zeros(B.tsd_paged_attention_workspace_bytes(pool.cache, Hq), dtype=torch.uint8, device=DEV)
+    out = torch.full_like(q, 3.0) if out is None else out
+    lse = torch.full((S, Hq), 3.0, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.tsd_paged_attention(pool.cache, q, lens, out, lse, sm_scale, workspace, status, stream)
+    return out, lse, status
+
+
+def _check_token(pool, q, lens, out, lse, sm_scale):
+    bits = 2.0 ** -22 if q.dtype == torch.float32 else 2.0 ** -16
+    for s, n in enumerate(lens):
+        k, v, qs = pool.dense("k", s, n), pool.dense("v", s, n), _np(q[s])
+        ref, ref_lse = oracle.token_attention(qs, k, v, sm_scale)
+        if n == 0:
+            assert not out[s].any() and bool(torch.isneginf(lse[s]).all())
+            continue
+        group = qs.shape[0] // k.shape[1]
+        for h in range(qs.shape[0]):
+            g = h // group
+            size = abs(sm_scale) * (np.abs(k[:, g]) @ np.abs(qs[h])).max()
+            off = (qs.shape[1] + 4) * 2.0 ** -24 * size                                # of a score
+            tol = HALF_STEP[q.dtype] * np.abs(ref[h]) + 2 * (off + bits) * np.abs(v[:, g]).max()
+            assert (np.abs(_np(out[s, h]) - ref[h]) <= tol).all(), (s, h, np.abs(_np(out[s, h]) - ref[h]).max())
+            assert abs(float(lse[s, h]) - ref_lse[h]) <= off + 2.0 ** -22 * (1 + abs(ref_lse[h]))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "e4m3"])
+@pytest.mark.parametrize("Hq,Hkv,d,page,lens", [
+    (32, 32, 128, 64, [768]), (28, 4, 128, 16, [0, 1, 2, 15, 16, 17, 300]), (4, 4, 64, 8, [7, 8, 9, 63, 64, 65, 0]), (8, 1, 64, 128, [1000, 0, 127]),
+    (2, 1, 128, 32, [31, 33, 1]), (16, 1, 128, 64, [500, 3]), (36, 4, 64, 16, [129, 40]), (40, 1, 128, 1024, [1, 1500]), (12, 3, 64, 256, [2000, 255, 257, 0])])
+def test_token_attention(kind, Hq, Hkv, d, page, lens):
+    # every type over head layouts (groups of 1 to 40) and lengths around chunks and pages; NaN wherever nothing may be read
+    gen = torch.Generator(device=DEV).manual_seed(Hq + page)
+    pool = Pool(kind, lens, Hkv, d, page, seed=page, head_major=page == 32, fill=lens)
+    q = _rnd(gen, len(lens), Hq, d, dtype=pool.dtype) * 2
+    out, lse, status = _token(pool, q, _i32(lens), d ** -0.5)
+    torch.cuda.synchronize()
+    assert status.item() == 0
+    _check_token(pool, q, lens, out, lse, d ** -0.5)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "e4m3"])
+def test_one_long_sequence_is_cut_and_joined(kind):
+    # one sequence over all blocks; the largest scores lie in one stretch, so that the others' parts weigh nothing
+    lens = [40000 if kind != "f32" else 20011]
+    pool = Pool(kind, lens, 2, 128, 64, fill=lens)
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    q = _rnd(gen, 1, 14, 128, dtype=pool.dtype)
+    for scale in (128 ** -0.5, 4.0, -0.3, 0.0):
+        out, lse, _ = _token(pool, q, _i32(lens), scale)
+        _check_token(pool, q, lens, out, lse, scale)
+
+
+def test_many_sequences_and_repeats():
+    # more sequences than blocks, many of them empty; the same call gives the same bits, in any workspace that has been used before
+    rng = np.random.default_rng(0)
+    lens = [int(x) for x in rng.integers(0, 90, 333)]
+    lens[::7] = [0] * len(lens[::7])
+    lens[100] = 5000
+    pool = Pool("bf16", lens, 2, 64, 16, fill=lens)
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    q = _rnd(gen, len(lens), 6, 64, dtype=torch.bfloat16)
+    ws = torch.zeros(B.tsd_paged_attention_workspace_bytes(pool.cache, 6), dtype=torch.uint8, device=DEV)
+    out, lse, _ = _token(pool, q, _i32(lens), 0.125, ws)
+    _check_token(pool, q, lens, out, lse, 0.125)
+    small = Pool("bf16", [70, 3], 2, 64, 16)
+    for _ in range(3):
+        _token(small, q[:2, :, :].contiguous(), _i32([70, 3]), 0.125, ws)
+        again, lse2, _ = _token(pool, q, _i32(lens), 0.125, ws)
+        assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+def test_all_empty_none_and_clamped_lengths():
+    pool = Pool("bf16", [64, 64, 64], 2, 64, 16)
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    q = _rnd(gen, 3, 4, 64, dtype=torch.bfloat16)
+    out, lse, _ = _token(pool, q, _i32([0, 0, -5]), 0.125)
+    assert not out.any() and bool(torch.isneginf(lse).all())
+    out, lse, _ = _token(pool, q, None, 0.125)
+    _check_token(pool, q, [64] * 3, out, lse, 0.125)
+    more, lse2, status = _token(pool, q, _i32([64, 1 << 30, 0x7fffffff]), 0.125)
+    assert torch.equal(out, more) and torch.equal(lse, lse2) and status.item() == 0
+
+
+def test_pages_that_do_not_exist_read_as_zeros():
+    lens = [100, 100, 100]
+    pool = Pool("bf16", lens, 2, 128, 16)
+    pool.table[1, 2], pool.table[2, 6] = -1, pool.cache.n_pages
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    q = _rnd(gen, 3, 4, 128, dtype=torch.bfloat16)
+    out, lse, status = _token(pool, q, _i32(lens), 0.1)
+    assert B.tsd_check_status(status) == B.TSD_ERR_DEVICE_DATA
+    _check_token(pool, q, lens, out, lse, 0.1)                                          # the oracle reads zeros there, too
+    pool.table[2, 6] = 0
+    lens = [100, 32, 96]                                                                # what is not needed is not looked at
+    out, lse, status = _token(pool, q, _i32(lens), 0.1)
+    assert status.item() == 0
+    _check_token(pool, q, lens, out, lse, 0.1)
+
+
+def test_e4m3_codes_are_read_exactly():
+    # every finite code as a value, selected one by one: a query that meets one key only, and one column per head
+    codes = [c for c in range(256) if c & 0x7F != 0x7F]
+    lens = [1] * len(codes)
+    pool = Pool("e4m3", lens, 1, 64, 8, fill=lens)
+    pool.scale["k"].fill_(1.0)
+    pool.scale["v"].fill_(1.0)
+    for s, c in enumerate(codes):
+        for x in "kv":
+            pool.pages[x].view(torch.uint8)[int(pool.table[s, 0]), 0] = c
+    q = torch.full((len(codes), 1, 64), 0.0, dtype=torch.bfloat16, device=DEV)
+    q[:, 0, 5] = 1.0
+    out, lse, _ = _token(pool, q, _i32(lens), 1.0)
+    want = torch.tensor(codes, dtype=torch.uint8).view(FP8).double()
+    assert torch.equal(out[:, 0].double().cpu(), want[:, None].expand(-1, 64))
+    assert (lse[:, 0].double().cpu() - want).abs().max() <= 2.0 ** -22 * 448
+
+
+def test_views_and_strides():
+    # queries out of a joint projection, an output with padded heads, pages whose K and V lie in one tensor
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    both = _rnd(gen, 12, 16, 4, 128, dtype=torch.bfloat16)
+    table = torch.randperm(12, generator=gen, device=DEV).to(torch.int32).view(2, 6)[:, :5]
+    cache = B.make_paged_cache(both[:, :, :2], both[:, :, 2:], table)
+    q = _rnd(gen, 2, 12, 128, dtype=torch.bfloat16)[:, 2:10]
+    out = torch.full((2, 8, 256), 5.0, dtype=torch.bfloat16, device=DEV)
+    ws = torch.zeros(B.tsd_paged_attention_workspace_bytes(cache, 8), dtype=torch.uint8, device=DEV)
+    B.tsd_paged_attention(cache, q, _i32([80, 41]), out[:, :, :128], None, 0.1, ws)
+    for s, n in enumerate([80, 41]):
+        rows = both[table[s].long()].flatten(0, 1)[:n]
+        ref, _ = oracle.token_attention(_np(q[s]), _np(rows[:, :2]), _np(rows[:, 2:]), 0.1)
+        assert np.abs(_np(out[s, :, :128]) - ref).max() <= 2.0 ** -8 * 5 + 1e-3
+    assert bool((out[:, :, 128:] == 5).all())
+
+
+def test_offsets_beyond_32_bits():
+    # pools of 4.6 GB each: the pages in use lie behind the 2^32nd byte
+    page, H, d, n_pages = 1024, 8, 128, 4500
+    pool = [torch.empty((n_pages, page, H, d), dtype=FP8, device=DEV) for _ in range(2)]
+    table = _i32([[4499, 4400, 2]])
+    cache = B.make_paged_cache(pool[0], pool[1], table)
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    k, v = [(_rnd(gen, 1, 2500, H, d) * 20).to(torch.bfloat16) for _ in range(2)]
+    B.tsd_append_paged_kv(cache, k, v)
+    q = _rnd(gen, 1, H, d, dtype=torch.bfloat16) * 0.1
+    out, ws = torch.empty_like(q), torch.zeros(B.tsd_paged_attention_workspace_bytes(cache, H), dtype=torch.uint8, device=DEV)
+    B.tsd_paged_attention(cache, q, _i32([2500]), out, None, 0.1, ws)
+    kd, vd = [_np(x.clamp(-448, 448).to(FP8)[0]) for x in (k, v)]
+    ref, _ = oracle.token_attention(_np(q[0]), kd, vd, 0.1)
+    assert np.abs(_np(out[0]) - ref).max() <= 2.0 ** -8 * np.abs(ref).max() + 1e-3 * np.abs(vd).max()
+
+
+def test_captured_calls_follow_their_inputs():
+    # append and attention in one graph, replayed while the cache grows token by token, on a stream of its own
+    S, H, d, page = 3, 4, 128, 16
+    start = [30, 0, 47]
+    pool = Pool("bf16", [a + 20 for a in start], H, d, page)
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    x = {n: torch.zeros((S, 1, H, d), dtype=torch.bfloat16, device=DEV) for n in "kvq"}
+    qr, out, lse = torch.zeros_like(x["q"]), torch.zeros((S, H, d), dtype=torch.bfloat16, device=DEV), torch.zeros((S, H), device=DEV)
+    slot, lens = _i32(start), _i32([a + 1 for a in start])
+    freq = torch.rand(64, generator=gen, device=DEV)
+    ws = torch.zeros(B.tsd_paged_attention_workspace_bytes(pool.cache, H), dtype=torch.uint8, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+
+    def token():
+        B.tsd_append_paged_kv(pool.cache, x["k"], x["v"], slot, inv_freq=freq, q=x["q"], q_out=qr, status=status)
+        B.tsd_paged_attention(pool.cache, qr[:, 0], lens, out, lse, 0.09, ws, status)
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        token()
+        stream.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            token()
+        for step in range(20):
+            for n in "kvq":
+                x[n].copy_(_rnd(gen, S, 1, H, d, dtype=torch.bfloat16))
+            graph.replay()
+            _check_token(pool, qr[:, 0], [a + 1 + step for a in start], out, lse, 0.09)
+            slot += 1
+            lens += 1
+        stream.synchronize()
+    assert status.item() == 0
+
+
+def test_two_calls_at_once_in_workspaces_of_their_own():
+    lens = [[3000, 77], [1234, 2048]]
+    pools = [Pool("bf16", n, 4, 128, 64, seed=i) for i, n in enumerate(lens)]
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    qs = [_rnd(gen, 2, 28, 128, dtype=torch.bfloat16) for _ in pools]
+    alone = [_token(p, q, _i32(n), 0.09)[:2] for p, q, n in zip(pools, qs, lens)]
+    streams = [torch.cuda.Stream() for _ in pools]
+    spaces = [torch.zeros(B.tsd_paged_attention_workspace_bytes(p.cache, 28), dtype=torch.uint8, device=DEV) for p in pools]
+    lt = [_i32(n) for n in lens]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(_token(pools[i], qs[i], lt[i], 0.09, spaces[i])[:2])
+    torch.cuda.synchronize()
+    for i in range(2):
+        for out, lse in got[i]:
+            assert torch.equal(out, alone[i][0]) and torch.equal(lse, alone[i][1])
+
+
+# ------------------------------------------------------------------------------------------ verify
+@pytest.mark.parametrize("flags", [0, B.TSD_ATTN_FORCE_SIMT])
+@pytest.mark.parametrize("kind", ["bf16", "f32", "e4m3"])
+@pytest.mark.parametrize("S,Bn,R,Nc,Hq,Hkv,d,page,lens", [
+    (1, 8, 32, 736, 32, 32, 128, 32, None), (3, 5, 32, 300, 28, 4, 128, 16, [300, 0, 17]), (2, 2, 64, 129, 4, 2, 64, 8, [129, 65]),
+    (2, 13, 32, 1100, 8, 8, 64, 64, [1100, 1]), (1, 3, 128, 1000, 2, 1, 128, 1024, None), (2, 4, 32, 500, 6, 1, 128, 128, [64, 500]),
+    (1, 1, 32, 5056, 4, 4, 128, 64, None), (2, 3, 32, 0, 2, 2, 128, 16, None)])
+def test_verify_over_pages_equals_verify_over_a_dense_cache(flags, kind, S, Bn, R, Nc, Hq, Hkv, d, page, lens):
+    if kind == "f32" and flags:
+        pytest.skip("fp32 takes the CUDA-core kernel anyway")
+    dt = TYPES[kind][0]
+    used = [Nc] * S if lens is None else lens
+    pool = Pool(kind, [max(Nc, 1)] * S, Hkv, d, page, seed=Nc, head_major=page == 32, fill=used)
+    for s, n in enumerate(used):                                                       # pages behind the length: not handed out
+        pool.table[s, -(-n // page):] = -1
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    q, kd, vd = _rnd(gen, S, Bn * R, Hq, d, dtype=dt), _rnd(gen, S, Bn * R, Hkv, d, dtype=dt), _rnd(gen, S, Bn * R, Hkv, d, dtype=dt)
+    dense = []
+    for name in "kv":
+        x = torch.zeros((S, max(Nc, 1), Hkv, d), dtype=torch.float64)
+        for s, n in enumerate(used):
+            x[s, :n] = torch.from_numpy(pool.dense(name, s, n))
+        dense.append(x.float().to(dt).to(DEV)[:, :Nc])
+    steps = [VerifyStep(S, Bn, R, Nc, Hq, Hkv, d, 64, 1, dt) for _ in range(2)]
+    for st in steps:
+        st.build_mask(None, None if lens is None else _i32(lens))
+        st.out.fill_(9.0)
+    a = steps[0].attention_paged(q, pool.cache, kd, vd, d ** -0.5, flags)
+    b = steps[1].attention(q, dense[0] if Nc else None, dense[1] if Nc else None, kd, vd, d ** -0.5, flags)
+    for st in steps:
+        st.check_status()
+    assert torch.equal(a, b) and torch.equal(steps[0].attn_lse, steps[1].attn_lse)
+    assert bool(torch.isfinite(a.float()).all())
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_verify_over_missing_pages(kind):
+    # in a tile of its own, in the middle of a tile and first of the block's items: zeros, and reported
+    S, Nc, page = 2, 400, 16
+    pool = Pool(kind, [Nc] * S, 2, 128, page)
+    pool.table[0, 0], pool.table[1, 9], pool.table[1, 24] = -1, pool.cache.n_pages, -7
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    q, kd, vd = [_rnd(gen, S, 64, h, 128, dtype=torch.bfloat16) for h in (4, 2, 2)]
+    steps = [VerifyStep(S, 2, 32, Nc, 4, 2, 128, 64, 1, torch.bfloat16) for _ in range(2)]
+    a = steps[0].attention_paged(q, pool.cache, kd, vd, 0.1)
+    dense = [torch.stack([torch.from_numpy(pool.dense(x, s, Nc)) for s in range(S)]).float().bfloat16().to(DEV) for x in "kv"]
+    b = steps[1].attention(q, dense[0], dense[1], kd, vd, 0.1)
+    assert torch.equal(a, b) and torch.equal(steps[0].attn_lse, steps[1].attn_lse)
+    assert B.tsd_check_status(steps[0].status) == B.TSD_ERR_DEVICE_DATA
+
+
+def test_verify_refusals_on_a_device():
+    pool = Pool("bf16", [64], 2, 128, 16)
+    step = VerifyStep(1, 1, 32, 64, 4, 2, 128, 64, 1, torch.bfloat16)
+    q, kd = [torch.zeros((1, 32, h, 128), dtype=torch.bfloat16, device=DEV) for h in (4, 2)]
+    with pytest.raises(B.TsdError):
+        step.attention_paged(q, pool.cache, kd, kd, 0.0)                                # the tensor-core kernel wants a positive scale
+    step.attention_paged(q, pool.cache, kd, kd, 0.0, B.TSD_ATTN_FORCE_SIMT)
+    for bad in ((q[:, :16], kd), (q.float(), kd), (q, kd[:, :, :1]), (q.cpu(), kd), (q, kd.float())):
+        with pytest.raises(AssertionError):
+            step.attention_paged(bad[0], pool.cache, bad[1], bad[1], 0.1)
+
+
+def test_refusals_of_the_binding():
+    pool = Pool("bf16", [64, 64], 2, 128, 16)
+    q = torch.zeros((2, 4, 128), dtype=torch.bfloat16, device=DEV)
+    ws = torch.zeros(B.tsd_paged_attention_workspace_bytes(pool.cache, 4), dtype=torch.uint8, device=DEV)
+    ok = dict(q=q, kv_lens=_i32([1, 2]), out=torch.empty_like(q), lse=torch.empty((2, 4), device=DEV), workspace=ws)
+    B.tsd_paged_attention(pool.cache, **ok)
+    for bad in (dict(q=q[:1]), dict(q=q.cpu()), dict(out=q[:, :2]), dict(out=torch.empty_like(q, dtype=torch.float32)), dict(kv_lens=_i32([1])),
+                dict(kv_lens=torch.tensor([1, 2], device=DEV)), dict(kv_lens=torch.tensor([1, 2], dtype=torch.int32)),
+                dict(lse=torch.empty((2, 3), device=DEV)), dict(lse=torch.empty((2, 4), device=DEV).bfloat16()), dict(q=q[:, :, :64], out=q[:, :, :64])):
+        with pytest.raises(AssertionError):
+            B.tsd_paged_attention(pool.cache, **dict(ok, **bad))
+    with pytest.raises(B.TsdError):
+        B.tsd_paged_attention(pool.cache, **dict(ok, workspace=ws[:64]))
+    with pytest.raises(B.TsdError):
+        B.tsd_paged_attention(pool.cache, **dict(ok, q=q.half()))
+    k = torch.zeros((2, 6, 2, 128), dtype=torch.bfloat16, device=DEV)
+    for bad in (dict(v=k[:, :5]), dict(v=k.float()), dict(n_rows=4), dict(q=k), dict(q_out=k), dict(q=k, q_out=k[:, :3]), dict(first_slot=_i32([1])),
+                dict(n_new=_i32([1, 2, 3])), dict(positions=_i32([1, 2])), dict(inv_freq=torch.zeros(8, dtype=torch.float64, device=DEV)),
+                dict(k_out=k[:, :, :1]), dict(v=k.cpu())):
+        with pytest.raises(AssertionError):
+            B.tsd_append_paged_kv(pool.cache, k, **dict(dict(v=k), **bad))
+    with pytest.raises(B.TsdError):
+        B.tsd_append_paged_kv(pool.cache, k, None)
+
+
+# ---------------------------------------------------------------------------------------- together
+def test_a_block_from_prompt_to_next_token():
+    """Prompts into pages, a tree's rows rotated, verified over the pages, its accepted node appended, and a token on top: every stage
+    against the same work on dense tensors."""
+    S, Bn, R, Hq, Hkv, d, page = 3, 4, 32, 8, 2, 128, 16
+    prompt = [70, 1, 200]
+    gen = torch.Generator(device=DEV).manual_seed(6)
+    pool = Pool("bf16", [n + R + 1 for n in prompt], Hkv, d, page, fill=[0] * S)
+    freq = (1e4 ** (-torch.arange(0, d, 2, device=DEV) / d)).float()
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    bf = torch.bfloat16
+    k, v = _rnd(gen, S, 200, Hkv, d, dtype=bf), _rnd(gen, S, 200, Hkv, d, dtype=bf)
+    B.tsd_append_paged_kv(pool.cache, k, v, n_new=_i32(prompt), inv_freq=freq, status=status)
+    q, kd, vd = _rnd(gen, S, Bn * R, Hq, d, dtype=bf), _rnd(gen, S, Bn * R, Hkv, d, dtype=bf), _rnd(gen, S, Bn * R, Hkv, d, dtype=bf)
+    pos = (_i32(prompt)[:, None] + torch.arange(R, device=DEV, dtype=torch.int32).repeat(Bn)).contiguous()
+    B.tsd_append_paged_kv(None, kd, None, positions=pos, inv_freq=freq, q=q, q_out=q, k_out=kd)
+    step = VerifyStep(S, Bn, R, 256, Hq, Hkv, d, 64, 1, bf)
+    cache = B.make_paged_cache(pool.pages["k"], pool.pages["v"], torch.nn.functional.pad(pool.table, (0, 16), value=-1))
+    step.build_mask(None, _i32(prompt))
+    out = step.attention_paged(q, cache, kd, vd, d ** -0.5)
+    rot = lambda x, p: torch.from_numpy(oracle.rotate(_np(x), np.asarray(p), _np(freq)))
+    for s, n in enumerate(prompt):
+        keys, values = rot(k[s, :n], np.arange(n)).numpy(), _np(v[s, :n])
+        for b in range(Bn):
+            mine = slice(b * R, (b + 1) * R)
+            kk, vv = np.concatenate([keys, _np(kd[s, mine])]), np.concatenate([values, _np(vd[s, mine])])
+            ref = np.stack([oracle.token_attention(_np(q[s, b * R + r]), kk, vv, d ** -0.5)[0] for r in (0, 31)])
+            assert np.abs(_np(out[s, [b * R, b * R + 31]]) - ref).max() <= 2e-2         # K of the prompt rounded to bf16, weights too
+    node = _i32([3, 0, 2])
+    B.tsd_append_paged_kv(cache, kd, vd, _i32(prompt), block=node, n_rows=R, status=status)
+    k1, v1, q1 = [_rnd(gen, S, 1, h, d, dtype=bf) for h in (Hkv, Hkv, Hq)]
+    B.tsd_append_paged_kv(cache, k1, v1, _i32([n + R for n in prompt]), inv_freq=freq, q=q1, q_out=q1, status=status)
+    lens = [n + R + 1 for n in prompt]
+    got, lse, _ = _token(pool, q1[:, 0], _i32(lens), d ** -0.5)
+    _check_token(pool, q1[:, 0], lens, got, lse, d ** -0.5)
+    for s, n in enumerate(prompt):                                                      # and the pages hold what was appended
+        b = int(node[s])
+        assert np.array_equal(pool.dense("k", s, lens[s])[n:n + R], _np(kd[s, b * R:(b + 1) * R]))
+        assert np.array_equal(pool.dense("v", s, lens[s]), np.concatenate([_np(v[s, :n]), _np(vd[s, b * R:(b + 1) * R]), _np(v1[s])]))
+    assert status.item() == 0
+    step.check_status()
