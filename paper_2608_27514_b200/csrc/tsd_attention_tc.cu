@@ -371,34 +371,17 @@ struct TcParams {
   int cut;                        // blocks per item (a cluster), each with a stretch of its key tiles; 1: whole items
   __nv_bfloat16* out;             // where cut items are written without a tensor map
   int64_t os_b, os_r, os_h;
-  const int32_t* table;           // cache in pages of 2^page_shift rows, n_pages of them
+};
+// Where the cached keys come from: one dense cache per sequence, or pages of 2^page_shift rows.
+struct TcDense {
+  static constexpr bool kPaged = false;
+};
+struct TcPages {
+  static constexpr bool kPaged = true;
+  const int32_t* table;
   int64_t table_stride;
   int page_shift, n_pages;
 };
-
-// A cached tile of 64 keys from its pages: a copy per page that it touches (per 64 rows of a larger one), each with a page as its
-// outermost coordinate.  Rows below `clen` only: behind it a page may not have been handed out, and the copy engine fills what lies outside the pool
-// with zeros.  So it does for an entry that is no page of the pool, which is reported (by the K producer).
-// `page0`: the first entry, asked for before the wait for the stage.
-template <int D>
-__device__ __forceinline__ void load_paged_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int g, int row, int clen, int page0,
-                                                const int32_t* entries, const TcParams& p, bool report) {
-  const int box = min(1 << p.page_shift, kKeys);
-  for (int r = 0; r < kKeys; r += box) {
-    const int key = row + r;
-    int page = -1;
-    if (key < clen) {
-      page = r == 0 ? page0 : entries[key >> p.page_shift];
-      if (page < 0 || page >= p.n_pages) {
-        page = -1;
-        if (report && p.status) atomicOr(p.status, TSD_STATUS_BAD_INDEX);
-      }
-    }
-    const int in_page = key & ((1 << p.page_shift) - 1);
-    tma_load_4d(dst + (uint32_t)r * 128u, map, bar, 0, g, in_page, page);
-    if (D == 128) tma_load_4d(dst + kSubKV + (uint32_t)r * 128u, map, bar, 64, g, in_page, page);
-  }
-}
 
 // The MMAs of a tile go out as ONE block of instructions: the issuing lane shares its scheduler with
 // three softmax warps, so every instruction between two MMAs (a predicate, a 64-bit add for a
@@ -535,12 +518,13 @@ __device__ __noinline__ void copy_q_row(uint32_t q_smem, int r, uint32_t t_q) {
   tmem_wait_st();
 }
 
-template <int D, bool kCut, bool kPaged>
+template <int D, bool kCut, typename Cache>
 __global__ void __launch_bounds__(kTcThreads, 1)
 attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_kc,
                     const __grid_constant__ CUtensorMap map_vc, const __grid_constant__ CUtensorMap map_kd,
                     const __grid_constant__ CUtensorMap map_vd, const __grid_constant__ CUtensorMap map_o,
-                    const TcParams p) {
+                    const TcParams p, const Cache pages) {
+  constexpr bool kPaged = Cache::kPaged;
   using L = TcSmem<D>;
   using C = TcCols<D>;
   constexpr uint32_t kTileBytes = L::kTileBytes, kKVBytes = L::kKVBytes;
@@ -631,8 +615,6 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                "@c fence.acq_rel.gpu;\n@c fence.proxy.async.global;\n@!c griddepcontrol.wait;\n"
                "@n fence.acq_rel.gpu;\n@n griddepcontrol.launch_dependents;\n}" ::"r"(p.concurrent), "r"(p.next_at_once) : "memory");
   settle(mask);
-  const int32_t* table = p.table;
-  if constexpr (kPaged) settle(table);
 
   const int h_magic = mask[H_MAGIC], h_s = mask[H_S], h_b = mask[H_B], h_r = mask[H_R], h_nc = mask[H_NC];
   // tile counts of this block's items (the blob's layout follows from the tsd_layout, so no
@@ -701,7 +683,107 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     // One warp streams the K tiles (and Q of the items to come), the other the V tiles: a lone
     // thread needs several hundred clocks per tile for its waits and copies, and K must run up to
     // four tiles ahead of V.
-    if (lane == 0) {
+    if constexpr (kPaged) {
+      // A cached tile is a copy per page that it touches (per 64 rows of a larger one), the page its outermost coordinate: lane i sees to
+      // the tile's i-th copy.  The lanes look up 32 entries at a time, of the tiles to come, and a whole set before it is needed: the way
+      // to L2 takes as long as a tile.
+      // Only what holds rows below the cache length is looked up; behind it a page may not have been handed out.  The copy engine fills what lies
+      // outside the pool with zeros, and so it does for an entry that is no page of the pool, which is reported.
+      const bool is_k = warp == kKProducerWarp;
+      bool ok = true;
+      int issued = 0, q_issued = (is_k && n_my > 0) ? 1 : 0;
+      auto issue_q = [&](bool block) {  // as below; lane 0 waits and copies, all lanes know
+        if (!ok || q_issued >= n_run) return;
+        const int x = q_issued;
+        const uint32_t b = bar(QT_READY + ((x - 1) & 1)), ph = ((x - 1) >> 1) & 1;
+        if (block) {
+          ok = mbar_wait(b, ph, abort_flag, 100);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) return;
+        } else if (!__all_sync(0xffffffffu, mbar_test_wait(b, ph))) {
+          return;
+        }
+        int s, h, qt;
+        item_coords(x, s, h, qt);
+        if (lane == 0) {
+          mbar_expect_tx(bar(QS_FULL), kTileBytes);
+          tma_load_4d(base + kOffQ, &map_q, bar(QS_FULL), 0, h, qt * kTile, s);
+          if (D == 128) tma_load_4d(base + kOffQ + kSub, &map_q, bar(QS_FULL), 64, h, qt * kTile, s);
+        }
+        __syncwarp();
+        q_issued = x + 1;
+      };
+      const CUtensorMap* mc = is_k ? &map_kc : &map_vc;
+      const CUtensorMap* md = is_k ? &map_kd : &map_vd;
+      const uint32_t stage0 = base + (is_k ? kOffK : kOffV);
+      const int full0 = is_k ? QK_GO : PV_GO, free0 = is_k ? K_FREE : PV_DONE;
+      const int n_stage = is_k ? kNK : kNV;
+      const int32_t* table = pages.table;
+      settle(table);
+      const int box = min(1 << pages.page_shift, kKeys), n_box = kKeys / box, set = 32 / n_box;  // a set: the copies of so many tiles
+      auto entries = [&](int s, int clen, int j) {  // of the set that begins at cached tile j, a copy per lane
+        const int key = j * kKeys + lane * box;
+        return key < clen ? table[s * pages.table_stride + (key >> pages.page_shift)] : -1;
+      };
+      auto first_entries = [&](int it, int j) { return entries(item_sg[it] / p.Hkv, item_clen[it], j); };
+      const int j0 = kCut ? *tile_first : 0;
+      int now = -1, ahead = n_run > 0 ? first_entries(0, j0) : -1;  // the set at hand, the one behind it
+      bool missing = false;
+      int G = 0, b = 0;
+      uint32_t ph = 0;
+      for (int it = 0; it < n_run && ok; ++it) {
+        while (is_k && ok && q_issued <= it) issue_q(true);
+        const int clen = item_clen[it];
+        const int s = item_sg[it] / p.Hkv, g = item_sg[it] - s * p.Hkv, n_ct = (clen + kKeys - 1) / kKeys, T = item_T[it];
+        const int32_t* rec = mask + item_rec[it];
+        if (n_ct <= j0 && it + 1 < n_run) ahead = first_entries(it + 1, 0);
+        for (int j = j0; j < j0 + T && ok; ++j, ++G) {
+          if (is_k) issue_q(false);
+          if (!ok) break;
+          if (G >= n_stage) {
+            ok = mbar_wait(bar(free0 + b), ph ^ 1u, abort_flag, 100);
+            ok = __all_sync(0xffffffffu, ok);
+          }
+          if (!ok) break;
+          const uint32_t dst = stage0 + b * kKVBytes, full_bar = bar(full0 + b);
+          if (lane == 0) {
+            mbar_expect_tx(full_bar, kKVBytes);
+            if (is_k && G < kNSb) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], 4;" ::"r"(full_bar) : "memory");
+          }
+          __syncwarp();
+          if (j < n_ct) {
+            const int in_set = (j - j0) % set;
+            if (in_set == 0) {
+              now = ahead;
+              if (j + set < min(n_ct, j0 + T)) ahead = entries(s, clen, j + set);
+              else if (it + 1 < n_run) ahead = first_entries(it + 1, 0);
+            }
+            int page = __shfl_sync(0xffffffffu, now, in_set * n_box + lane);
+            if (lane < n_box) {
+              const int key = j * kKeys + lane * box, in_page = key & ((1 << pages.page_shift) - 1);
+              const bool there = page >= 0 && page < pages.n_pages;
+              missing |= key < clen && !there;
+              if (!there) page = -1;
+              tma_load_4d(dst + (uint32_t)(lane * box) * 128u, mc, full_bar, 0, g, in_page, page);
+              if (D == 128) tma_load_4d(dst + kSubKV + (uint32_t)(lane * box) * 128u, mc, full_bar, 64, g, in_page, page);
+            }
+          } else if (lane == 0) {
+            const int row = rec[2 + 2 * (j - n_ct)] * kKeys;
+            tma_load_4d(dst, md, full_bar, 0, g, row, s);
+            if (D == 128) tma_load_4d(dst + kSubKV, md, full_bar, 64, g, row, s);
+          }
+          __syncwarp();
+          issued = G + 1;
+          if (++b == n_stage) { b = 0; ph ^= 1u; }
+        }
+      }
+      if (missing && is_k && p.status) atomicOr(p.status, TSD_STATUS_BAD_INDEX);
+      if (*abort_flag || n_run == 0) {  // as below
+        volatile uint32_t* scratch = abort_flag + 1;
+        if (q_issued > 0) mbar_wait(bar(QS_FULL), (q_issued - 1) & 1, scratch);
+        for (int t = max(0, issued - n_stage); t < issued; ++t) mbar_wait(bar(full0 + t % n_stage), (t / n_stage) & 1, scratch);
+      }
+    } else if (lane == 0) {
       const bool is_k = warp == kKProducerWarp;
       bool ok = true;
       int issued = 0, q_issued = (is_k && n_my > 0) ? 1 : 0;
@@ -737,14 +819,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         const uint32_t dst = stage0 + t * kKVBytes, full_bar = bar(full0 + t);
         mbar_expect_tx(full_bar, kKVBytes);
         if (is_k && t < kNSb) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], 4;" ::"r"(full_bar) : "memory");
-        if constexpr (kPaged) {
-          const int32_t* entries = table + s_first * p.table_stride;
-          load_paged_tile<D>(dst, mc, full_bar, g_first, (t_first + t) * kKeys, item_clen[0], entries[(t_first + t) * kKeys >> p.page_shift],
-                             entries, p, is_k);
-        } else {
         tma_load_4d(dst, mc, full_bar, 0, g_first, (t_first + t) * kKeys, s_first);
         if (D == 128) tma_load_4d(dst + kSubKV, mc, full_bar, 64, g_first, (t_first + t) * kKeys, s_first);
-        }
       }
       issued = n_pre;
       for (int it = 0; it < n_run && ok; ++it) {
@@ -756,9 +832,6 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         for (int j = j0; j < j0 + T && ok; ++j, ++G) {
           if (is_k) issue_q(false);
           if (!ok) break;
-          int page0 = 0;
-          if constexpr (kPaged)
-            if (j < n_ct) page0 = table[s * p.table_stride + (j * kKeys >> p.page_shift)];
           // the stage is free once the MMAs that read its previous tile have completed
           if (G >= n_stage) ok = mbar_wait(bar(free0 + b), ph ^ 1u, abort_flag, 100);
           if (!ok) break;
@@ -770,12 +843,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
             mbar_expect_tx(full_bar, kKVBytes);
             // no softmax has run before the first three tiles: their S buffers are free from the start
             if (is_k && G < kNSb) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], 4;" ::"r"(full_bar) : "memory");
-            if (kPaged && cached) {
-              load_paged_tile<D>(dst, m, full_bar, g, row, item_clen[it], page0, table + s * p.table_stride, p, is_k);
-            } else {
             tma_load_4d(dst, m, full_bar, 0, g, row, s);
             if (D == 128) tma_load_4d(dst + kSubKV, m, full_bar, 64, g, row, s);
-            }
             issued = G + 1;
           }
           TSD_TR(is_k ? 0 : 1, G);
@@ -1422,15 +1491,15 @@ bool attention_tc_supported(const AttnArgs& a) {
 size_t attention_tc_workspace_bytes(const tsd_layout&) { return 0; }
 
 // The kernels' dynamic shared memory limit, an attribute per device; needed by launches and by questions about them.
-template <int D, bool kPaged>
+template <int D, typename Cache>
 static cudaError_t allow_smem(int dev) {
   static std::mutex mu;
   static bool done[kMaxDevices];
   std::lock_guard<std::mutex> lock(mu);
   if (done[dev]) return cudaSuccess;
-  cudaError_t e = cudaFuncSetAttribute(attention_tc_kernel<D, false, kPaged>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcSmem<D>::kBytes);
+  cudaError_t e = cudaFuncSetAttribute(attention_tc_kernel<D, false, Cache>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcSmem<D>::kBytes);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(attention_tc_kernel<D, true, kPaged>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcSmem<D>::kBytes);
+    e = cudaFuncSetAttribute(attention_tc_kernel<D, true, Cache>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcSmem<D>::kBytes);
   done[dev] = e == cudaSuccess;
   return e;
 }
@@ -1443,7 +1512,7 @@ static int cut_items(int64_t n_items, int T) {
   static std::mutex mu;
   static int clusters[kMaxDevices][9];  // clusters of that many blocks that run at one time, + 1; 0: not asked yet
   const int dev = current_device();
-  if (dev < 0 || allow_smem<D, false>(dev) != cudaSuccess) return 1;
+  if (dev < 0 || allow_smem<D, TcDense>(dev) != cudaSuccess) return 1;
   std::lock_guard<std::mutex> lock(mu);
   int best = 1, best_time = T;  // in key tiles
   for (int n = 2, meet = kMeetTiles; n <= (D == 128 ? 8 : 4); n *= 2, meet += 2) {
@@ -1462,7 +1531,7 @@ static int cut_items(int64_t n_items, int T) {
       cfg.attrs = &attr;
       cfg.numAttrs = 1;
       int found = 0;
-      if (cudaOccupancyMaxActiveClusters(&found, attention_tc_kernel<D, true, false>, &cfg) != cudaSuccess) {
+      if (cudaOccupancyMaxActiveClusters(&found, attention_tc_kernel<D, true, TcDense>, &cfg) != cudaSuccess) {
         cudaGetLastError();
         return best;  // asked again next time
       }
@@ -1490,8 +1559,9 @@ int attention_tc_blocks(const tsd_layout& L) {
   return (int)n_items * (L.head_dim == 64 ? blocks_per_item<64>(L) : blocks_per_item<128>(L));
 }
 
-template <int D, bool kPaged>
+template <int D, typename Cache>
 static int launch_tc(const AttnArgs& a) {
+  constexpr bool kPaged = Cache::kPaged;
   const tsd_layout& L = a.L;
   const int N = L.n_branches * L.rows_per_branch;
   CUtensorMap mq, mkc, mvc, mkd, mvd, mo;
@@ -1517,7 +1587,7 @@ static int launch_tc(const AttnArgs& a) {
     return kPaged ? TSD_ERR_UNSUPPORTED : launch_attention_simt(a);
   const int dev = current_device();
   if (dev < 0) return cuda_fail(cudaErrorInvalidDevice, "cudaGetDevice");
-  const cudaError_t attr_err = allow_smem<D, kPaged>(dev);
+  const cudaError_t attr_err = allow_smem<D, Cache>(dev);
   if (attr_err != cudaSuccess) return cuda_fail(attr_err, "cudaFuncSetAttribute(attention_tc_kernel)");
   TcParams p;
   p.mask = a.mask;
@@ -1536,13 +1606,11 @@ static int launch_tc(const AttnArgs& a) {
   p.cut = blocks_per_item<D>(L);
   p.out = static_cast<__nv_bfloat16*>(a.out);
   p.os_b = a.os_b; p.os_r = a.os_r; p.os_h = a.os_h;
-  p.table = kPaged ? a.pages->table : nullptr;
-  p.table_stride = kPaged ? a.pages->table_stride : 0;
-  p.page_shift = kPaged ? a.pages->shift : 0;
-  p.n_pages = kPaged ? a.pages->n_pages : 0;
+  Cache pages;
+  if constexpr (kPaged) pages = TcPages{a.pages->table, a.pages->table_stride, a.pages->shift, a.pages->n_pages};
   if (p.cut > 1) {
-    cudaError_t e = launch_clusters(p.cut, attention_tc_kernel<D, true, kPaged>, (unsigned)(n_items * p.cut), kTcThreads, TcSmem<D>::kBytes, a.stream,
-                                    mq, mkc, mvc, mkd, mvd, mo, p);
+    cudaError_t e = launch_clusters(p.cut, attention_tc_kernel<D, true, Cache>, (unsigned)(n_items * p.cut), kTcThreads, TcSmem<D>::kBytes, a.stream,
+                                    mq, mkc, mvc, mkd, mvd, mo, p, pages);
     return e != cudaSuccess ? cuda_fail(e, "attention_tc_kernel") : TSD_OK;
   }
   // One block per SM, each walking its share of the items.  Where a share would not fit the block's item table, whole rounds of blocks: with
@@ -1550,15 +1618,15 @@ static int launch_tc(const AttnArgs& a) {
   // items of 8 tiles on 148 SMs: 1.56 and 2.71-2.83 ms; in whole rounds 1.56 and 1.59).
   const int64_t sms = std::max(device_facts().sms, 1);
   const int64_t grid = std::min(n_items, sms * ((n_items + sms * kMaxItems - 1) / (sms * kMaxItems)));
-  cudaError_t e = launch(attention_tc_kernel<D, false, kPaged>, (unsigned)grid, kTcThreads, TcSmem<D>::kBytes, a.stream, mq, mkc, mvc, mkd,
-                         mvd, mo, p);
+  cudaError_t e = launch(attention_tc_kernel<D, false, Cache>, (unsigned)grid, kTcThreads, TcSmem<D>::kBytes, a.stream, mq, mkc, mvc, mkd,
+                         mvd, mo, p, pages);
   if (e != cudaSuccess) return cuda_fail(e, "attention_tc_kernel");
   return TSD_OK;
 }
 
 int launch_attention_tc(const AttnArgs& a) {
-  if (a.pages) return a.L.head_dim == 64 ? launch_tc<64, true>(a) : launch_tc<128, true>(a);
-  return a.L.head_dim == 64 ? launch_tc<64, false>(a) : launch_tc<128, false>(a);
+  if (a.pages) return a.L.head_dim == 64 ? launch_tc<64, TcPages>(a) : launch_tc<128, TcPages>(a);
+  return a.L.head_dim == 64 ? launch_tc<64, TcDense>(a) : launch_tc<128, TcDense>(a);
 }
 
 }  // namespace tsd

@@ -1,36 +1,40 @@
 // Attention of one new token per sequence over a paged K/V cache (no counterpart in the paper, whose passes verify whole blocks:
 // tsd_verify_attention).  With q the query rows of the heads that share a kv head,
-//     s_t = sm_scale <q, k_t>,   out = sum_t e^(s_t - m) v_t / sum_t e^(s_t - m),   m = max_t s_t.
+//     s_t = sm_scale <q, k_t>,   out = sum_t e^(s_t - m) v_t / sum_t e^(s_t - m),   m >= max_t s_t - 8 log 2.
 // Every cached row is read once and used for a few multiply-adds per head, so the kernel is bound by memory; everything in it
-// serves to keep loads in flight.
+// serves to keep loads in flight and the work behind them short.
 //   split   : the keys of all sequences and heads are laid end to end in chunks of 4 KB of K and 4 KB of V (16 keys of 128 bf16) and cut
 //             evenly over the blocks, one per SM, whatever the single lengths are.  Inside a block the warps take the chunks in turn.
-//   warp    : a chunk goes from memory straight into the registers of one warp, in the layout that the matrix instruction wants.  For scores,
-//             lane (g, t) = (lane / 4, lane % 4) reads 16 bytes of key g at offsets 64 c + 16 t; which dimensions a step of the
-//             contraction takes is arbitrary as long as q is laid out alike, so these bytes are the B operand as they are.
-//             For the weighted sum, lane (g, t) reads columns 8 g ... of keys 2t, 2t+1, 2t+8, 2t+9 and pairs the keys' halves
-//             (one byte permutation per operand register).  K of the next chunk is requested as soon as the scores have used this one's, V likewise.
-//   rows    : mma.sync m16n8k16, rows = heads.  Up to 8 heads share a kv head: the other 8 rows carry the residuals of the weights,
-//             p - bf16(p), so that the weights count with 16 bits at no cost.  9 to 16 heads: a second product for the residuals.  More: tiles of 16 heads.
-//             The tensor memory instructions would bring 128-row tiles, of which 1 to 16 rows would be used, and a trip through shared memory.
-//   fp32    : the same loads on CUDA cores (the scores' partial sums of a key meet over its 4 lanes, the weights in shared memory).
-//   join    : at the end of a sequence's stretch the warps' running maxima, sums and rows meet in shared memory; a stretch that is not
+//   queue   : every warp has its next chunk on the way to shared memory while it works on one (cp.async: 128 KB per SM), and waits for
+//             its own fetches only, never for another warp.
+//   products: mma.sync m16n8k16 with K (16 keys) or V^T (16 dimensions) as the 16 rows and the heads as the 8 columns: no part of a product is
+//             wasted on 8 heads, and O takes 32 registers.  Which dimensions a step of the contraction takes is arbitrary as long as q is
+//             laid out alike: lane (g, t) = (lane / 4, lane % 4) reads 16 bytes of keys g and g + 8 at offset 64 c + 16 t, and these bytes
+//             are the operand as they are.  For V^T the lane reads columns 8 g ... of keys 2t, 2t+1, 2t+8, 2t+9 and pairs the keys'
+//             halves (a byte permutation per register).  Weights go from the one layout to the other by movmatrix, in two
+//             16-bit parts (high, residual: 2^-17 relative).  8-bit codes become f16, one conversion per pair.  The tensor-memory
+//             instructions would want 128 rows, and the scores back through tensor memory.
+//   offset  : m moves only when a score passes it by 8 (in the exp2 domain): one vote per chunk instead of a reduction.
+//   fp32    : the same queue on CUDA cores (the scores' partial sums of a key meet over its 4 lanes, the weights in shared memory).
+//   join    : at the end of a sequence's stretch the warps' offsets, sums and rows meet in shared memory; a stretch that is not
 //             the whole of its sequence goes to the workspace, and the last of its blocks to arrive puts the parts together, in their order.
 // Lengths are read on the device: a captured call follows them.  Rows past a length are not loaded.
+#include <cuda_fp16.h>
 #include <algorithm>
 #include <math_constants.h>
+#include <mutex>
 #include "tsd_paged.cuh"
 
 namespace tsd {
 
 constexpr int kTokenBlocks = kPlanSms;  // at most: what the workspace is sized for
-constexpr int kMinRounds = 2;           // chunks per warp that a block is worth
+constexpr float kSlack = 8.f;           // by how much a score may pass the offset, as a power of 2
 
 enum { kTypeF32 = TSD_F32, kTypeBf16 = TSD_BF16, kTypeE4m3 = TSD_E4M3 };
 
-template <int D, int kType, int HT>
+template <int D, int kType, int HT>  // HT: heads per tile, 8 or 16
 struct TokenPlan {
-  static constexpr int kWarps = 8;                                             // two per scheduler: up to 255 registers per thread
+  static constexpr int kWarps = HT == 8 ? 16 : 12;                             // at 128 and 168 registers a thread
   static constexpr int kSize = kType == kTypeF32 ? 4 : kType == kTypeBf16 ? 2 : 1;  // bytes of a cached element
   static constexpr int kRow = D * kSize;                                       // bytes of a row
   static constexpr int kPieces = kRow / 64;                                    // 16-byte pieces per lane and key
@@ -38,6 +42,9 @@ struct TokenPlan {
   static constexpr int kKeys = 8 * kGroups;                                    // keys per chunk
   static constexpr int kSlot = HT * D + 2 * HT;                                // floats of a part in the workspace
   static constexpr int kPitch = D + 4;                                         // floats between rows in shared memory
+  // dynamic shared memory: the warps' queues (a chunk's K, its V), then the warps' parts
+  static constexpr int kQueue = kWarps * 8192;
+  static constexpr int kBytes = kQueue + kWarps * 8 * kPitch * 4;
 };
 
 struct TokenParams {
@@ -64,35 +71,57 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-// 16 (8) bytes of the cache, or zeros; read once, so L1 keeps nothing of them.
-__device__ __forceinline__ uint4 load16(const uint8_t* p, bool wanted) {
-  uint4 v;
-  asm volatile("{\n.reg .pred w;\nsetp.ne.b32 w, %5, 0;\nmov.b32 %0, 0;\nmov.b32 %1, 0;\nmov.b32 %2, 0;\nmov.b32 %3, 0;\n"
-               "@w ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];\n}"
-               : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(p), "r"((int)wanted));
-  return v;
-}
-__device__ __forceinline__ uint2 load8(const uint8_t* p, bool wanted) {
-  uint2 v;
-  asm volatile("{\n.reg .pred w;\nsetp.ne.b32 w, %3, 0;\nmov.b32 %0, 0;\nmov.b32 %1, 0;\n"
-               "@w ld.global.nc.L1::no_allocate.v2.b32 {%0, %1}, [%2];\n}"
-               : "=&r"(v.x), "=&r"(v.y) : "l"(p), "r"((int)wanted));
-  return v;
-}
-__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-// Two e4m3 codes, in the upper bytes of the two halves of w, as bf16.  Sign, exponent and mantissa move to the places that bf16 has for them;
-// the value is then 2^-120 of what the code stands for (its smallest ones a subnormal bf16), and the product with 2^120 is exact.
-__device__ __forceinline__ uint32_t widen_e4m3(uint32_t w) {
-  const uint32_t x = ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u);
+__device__ __forceinline__ uint32_t f16_pair(float lo, float hi) {
   uint32_t r;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(0x7b807b80u));
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// A pair of weights as two 16-bit numbers, and what is left of them.
+template <bool kF16>
+__device__ __forceinline__ void split_pair(float x, float y, uint32_t& pair, uint32_t& rest) {
+  if constexpr (kF16) {
+    pair = f16_pair(x, y);
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&pair));
+    rest = f16_pair(x - f.x, y - f.y);
+  } else {
+    pair = bf16_pair(x, y);
+    rest = bf16_pair(x - __uint_as_float(pair << 16), y - __uint_as_float(pair & 0xffff0000u));
+  }
+}
+// 16 bytes of the cache, or zeros, into shared memory, asynchronously.
+__device__ __forceinline__ void fetch16(uint32_t to, const uint8_t* p, bool wanted) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(p), "r"(wanted ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void fetch_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void fetch_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+template <bool kF16>
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (kF16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// lane (g, t) has elements (g, 2t), (g, 2t + 1) of an 8 x 8 matrix, and gets (2t, g), (2t + 1, g)
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+// Two e4m3 codes, the lower (upper) half of w, as f16: exact.
+__device__ __forceinline__ uint32_t widen_lo(uint32_t w) {
+  uint32_t r;
+  asm("{\n.reg .b16 l, h;\nmov.b32 {l, h}, %1;\ncvt.rn.f16x2.e4m3x2 %0, l;\n}" : "=r"(r) : "r"(w));
+  return r;
+}
+__device__ __forceinline__ uint32_t widen_hi(uint32_t w) {
+  uint32_t r;
+  asm("{\n.reg .b16 l, h;\nmov.b32 {l, h}, %1;\ncvt.rn.f16x2.e4m3x2 %0, h;\n}" : "=r"(r) : "r"(w));
   return r;
 }
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
-__device__ __forceinline__ uint32_t word(const uint2& v, int i) { return i == 0 ? v.x : v.y; }
 
 // Where a chunk lies: sequence, head tile of the sequence, chunk; chunks and keys of the sequence.
 struct Cursor {
@@ -102,10 +131,12 @@ struct Cursor {
 template <int D, int kType, int HT>
 __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged_attention_kernel(const TokenParams p) {
   using P = TokenPlan<D, kType, HT>;
-  constexpr int NW = P::kWarps, KC = P::kKeys, NG = P::kGroups, NP = P::kPieces;
-  constexpr bool kF32 = kType == kTypeF32;
-  constexpr int kAcc = kF32 ? HT : D / 8;             // rows of 4 dimensions (fp32), or column blocks of 8
-  __shared__ __align__(16) float part_o[NW][8][P::kPitch];
+  constexpr int NW = P::kWarps, KC = P::kKeys, NG = P::kGroups, NP = P::kPieces, NT = HT / 8;
+  constexpr bool kF32 = kType == kTypeF32, kF16 = kType == kTypeE4m3;  // e4m3 is a subset of f16
+  constexpr int kTiles = D / 16;                       // of 16 dimensions
+  constexpr int kAcc = kF32 ? HT : kTiles * NT;        // rows of 4 dimensions (fp32), or tiles of 16 dimensions x 8 heads
+  extern __shared__ __align__(16) uint8_t dynamic[];
+  float (*part_o)[8][P::kPitch] = reinterpret_cast<float (*)[8][P::kPitch]>(dynamic + P::kQueue);
   __shared__ float part_m[NW][8], part_l[NW][8];
   __shared__ __align__(16) float weights[kF32 ? NW : 1][kF32 ? KC : 1][HT];
   __shared__ __align__(16) float q_rows[kF32 ? HT : 1][kF32 ? D : 1];
@@ -118,44 +149,45 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   auto length = [&](int s) { return a.lens ? min(max(a.lens[s], 0), a.cache.cap) : a.cache.cap; };
   auto chunks = [&](int len) { return (int)(((unsigned)len + KC - 1) / KC); };
 
-  // ---- this block's share [x0, x1) of all chunks
-  int64_t total = 0;
+  // ---- this block's share [x0, x1) of all chunks (fewer than 2^30: checked on the host)
+  int total = 0;
+  const int len0 = lane < a.S ? length(lane) : 0;  // of the first 32 sequences
   for (int s = lane; s < a.S; s += 32) {
-    const int n = chunks(length(s));
+    const int n = chunks(s < 32 ? len0 : length(s));
     total += n;
-    if (n == 0 && s % (int)gridDim.x == (int)blockIdx.x) {  // a sequence without keys (the lanes of warp 0 write what its rows are)
-      if (warp == 0)
-        for (int h = 0; h < a.Hq; ++h) {
-          if (a.lse) a.lse[(int64_t)s * a.Hq + h] = -CUDART_INF_F;
-          uint4* o = reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.out) + (s * a.o_b + h * a.o_h) * (kF32 ? 4 : 2));
-          for (int i = 0; i < D * (kF32 ? 4 : 2) / 16; ++i) o[i] = make_uint4(0, 0, 0, 0);
-        }
+    if (n == 0 && s % (int)gridDim.x == (int)blockIdx.x && warp == 0) {  // a sequence without keys
+      for (int h = 0; h < a.Hq; ++h) {
+        if (a.lse) a.lse[(int64_t)s * a.Hq + h] = -CUDART_INF_F;
+        uint4* o = reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.out) + (s * a.o_b + h * a.o_h) * (kF32 ? 4 : 2));
+        for (int i = 0; i < D * (kF32 ? 4 : 2) / 16; ++i) o[i] = make_uint4(0, 0, 0, 0);
+      }
     }
   }
 #pragma unroll
   for (int off = 16; off >= 1; off >>= 1) total += __shfl_xor_sync(full, total, off);
   total *= HI;
-  const int64_t n_blocks = min((int64_t)gridDim.x, (total + NW * kMinRounds - 1) / (NW * kMinRounds));
-  if ((int64_t)blockIdx.x >= n_blocks) return;
+  const int n_blocks = min((int)gridDim.x, (total + NW - 1) / NW);
+  if ((int)blockIdx.x >= n_blocks) return;
   // blocks take total / n_blocks chunks each, the first `more` of them one more
-  const int64_t each = total / n_blocks, more = total % n_blocks;
-  auto first_of = [&](int64_t b) { return b * each + min(b, more); };
-  auto block_of = [&](int64_t x) { return x < more * (each + 1) ? x / (each + 1) : more + (x - more * (each + 1)) / each; };
-  const int64_t x0 = first_of(blockIdx.x), x1 = first_of(blockIdx.x + 1);
+  const int each = total / n_blocks, more = total - each * n_blocks;
+  auto first_of = [&](int b) { return b * each + min(b, more); };
+  auto block_of = [&](int x) { return x < more * (each + 1) ? x / (each + 1) : more + (x - more * (each + 1)) / each; };
+  const int x0 = first_of(blockIdx.x), x1 = first_of(blockIdx.x + 1);
 
   // ---- where chunk x0 lies
-  Cursor seg;  // of the block's stretch at hand
-  int64_t seg_first;  // first chunk of its (sequence, head tile)
+  Cursor seg;     // of the block's stretch at hand
+  int seg_first;  // first chunk of its (sequence, head tile)
   {
-    int64_t before = 0;
-    seg.s = a.S;
+    int before = 0;
+    seg.s = 0;
+    seg.len = 0;
     for (int s0 = 0; s0 < a.S; s0 += 32) {
-      const int len = s0 + lane < a.S ? length(s0 + lane) : 0;
-      const int64_t mine = (int64_t)chunks(len) * HI;
-      int64_t upto = mine;
+      const int len = s0 == 0 ? len0 : s0 + lane < a.S ? length(s0 + lane) : 0;
+      const int mine = chunks(len) * HI;
+      int upto = mine;
 #pragma unroll
       for (int off = 1; off < 32; off <<= 1) {
-        const int64_t o = __shfl_up_sync(full, upto, off);
+        const int o = __shfl_up_sync(full, upto, off);
         if (lane >= off) upto += o;
       }
       const unsigned hit = __ballot_sync(full, before + upto > x0);
@@ -169,101 +201,92 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
       before += __shfl_sync(full, upto, 31);
     }
     seg.n = chunks(seg.len);
-    seg.hi = (int)((x0 - before) / seg.n);
-    seg.c = (int)((x0 - before) % seg.n);
+    seg.hi = (x0 - before) / seg.n;
+    seg.c = (x0 - before) - seg.hi * seg.n;
     seg_first = x0 - seg.c;
   }
-  auto next_sequence = [&](Cursor& cur) {
-    cur.hi = 0;
-    do {
-      if (++cur.s >= a.S) {  // behind the last chunk: never loaded
-        cur.n = 0x7fffffff;
-        cur.len = 0;
-        return;
-      }
-      cur.len = length(cur.s);
-      cur.n = chunks(cur.len);
-    } while (cur.n == 0);
-  };
   auto advance = [&](Cursor& cur, int step) {
     cur.c += step;
     while (cur.c >= cur.n) {
       cur.c -= cur.n;
-      if (++cur.hi == HI) next_sequence(cur);
+      if (++cur.hi == HI) {
+        cur.hi = 0;
+        do {
+          if (++cur.s >= a.S) {  // behind the last chunk: never fetched
+            cur.n = 0x7fffffff;
+            cur.len = 0;
+            break;
+          }
+          cur.len = length(cur.s);
+          cur.n = chunks(cur.len);
+        } while (cur.n == 0);
+      }
     }
   };
 
-  bool bad_page = false;
   const int row_mask = (1 << a.cache.shift) - 1;
-  // lane l < NG: the page of the chunk's keys [8 l, 8 l + 8), or -1
-  auto pages_of = [&](const Cursor& cur) {
-    const int key = cur.c * KC + 8 * lane;
-    int page = -1;
-    if (lane < NG && key < cur.len) {
-      page = page_of(a.cache, cur.s, key);
-      if (page < 0) bad_page = true;
-    }
-    return page;
+  const int64_t row_bytes = a.cache.ps_r * P::kSize, page_bytes = a.cache.ps_p * P::kSize, head_bytes = a.cache.ps_h * P::kSize;
+  // lane i < NG: the table's entry for the chunk's keys [8 i, 8 i + 8)
+  auto entry_of = [&](const Cursor& c) {
+    const int key = c.c * KC + 8 * lane;
+    return lane < NG && key < c.len ? a.cache.table[c.s * a.cache.table_stride + (key >> a.cache.shift)] : -1;
   };
-  uint4 kr[8];
-  uint4 vr[8];
-  const int64_t row_bytes = a.cache.ps_r * P::kSize;
-  auto load_k = [&](const Cursor& cur, int pages) {
-    const int key0 = cur.c * KC;
-    const uint8_t* base = static_cast<const uint8_t*>(a.cache.k) + (cur.hi / a.tiles) * (a.cache.ps_h * P::kSize) + 16 * t;
-#pragma unroll
-    for (int nb = 0; nb < NG; ++nb) {
-      const int page = __shfl_sync(full, pages, nb), key = key0 + 8 * nb + g;
-      const uint8_t* row = base + (int64_t)page * (a.cache.ps_p * P::kSize) + (key & row_mask) * row_bytes;
-#pragma unroll
-      for (int c = 0; c < NP; ++c) kr[nb * NP + c] = load16(row + 64 * c, page >= 0 && key < cur.len);
-    }
+  // What fetching a chunk takes: lane i < NG, where its 8 keys begin (from k or v on), or -1 where there is no page; how many keys count.
+  struct Place {
+    int64_t at;
+    int left;
   };
-  // bf16 and e4m3: keys 16 sub + {2t, 2t+1, 2t+8, 2t+9}; fp32: whole rows, a warp (or half of one) per key
-  auto load_v = [&](const Cursor& cur, int pages) {
-    const int key0 = cur.c * KC;
-    const uint8_t* base = static_cast<const uint8_t*>(a.cache.v) + (cur.hi / a.tiles) * (a.cache.ps_h * P::kSize);
-    if constexpr (kF32) {
+  bool bad_page = false;
+  auto place_of = [&](const Cursor& c, int entry) {
+    Place f;
+    f.left = c.len - c.c * KC;
+    const bool there = entry >= 0 && entry < a.cache.n_pages;
+    bad_page |= lane < NG && 8 * lane < f.left && !there;
+    const int key = c.c * KC + 8 * lane;
+    f.at = there ? (int64_t)entry * page_bytes + (int64_t)(key & row_mask) * row_bytes + (int64_t)(c.hi / a.tiles) * head_bytes : -1;
+    return f;
+  };
+  // The warp's queue: 4 KB of K, 4 KB of V.  They are fetched along the rows (an instruction that touches whole 128-byte lines: in the order
+  // in which the lanes want V, 32 bytes of a line at a time, the same loop without any arithmetic reads 5.0 TB/s instead of
+  // 6.9) and read back in the products' order, 16-byte pieces of a 128-byte line exchanged by row so that both orders of reading are free
+  // of bank conflicts (8 lanes read 4 pieces of 2 rows of K, 2 pieces of 4 rows of V).
+  constexpr int kLine = P::kRow / 16, kRowsAtOnce = 32 / kLine;  // pieces per row, rows per instruction
+  auto swizzle = [](int row) { return P::kRow == 64 ? (row >> 1) & 3 : ((row ^ (row >> 1)) & 1) << 2 | ((row >> 2) & 1) << 1; };
+  uint8_t* const queue = dynamic + warp * 8192;
+  const uint32_t queue_at = (uint32_t)__cvta_generic_to_shared(queue);
+  const int my_row = lane / kLine, my_piece = lane % kLine;
+  const int64_t lane_at = my_row * row_bytes + 16 * my_piece;
+  auto fetch = [&](const Place& f, const void* pages, uint32_t to) {
+    const uint8_t* base = static_cast<const uint8_t*>(pages);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int in = D == 128 ? i : 2 * i + (lane >> 4), key = key0 + in;
-        const int page = __shfl_sync(full, pages, in >> 3);
-        vr[i] = load16(base + (int64_t)page * (a.cache.ps_p * 4) + (key & row_mask) * row_bytes + 16 * (D == 128 ? lane : lane & 15),
-                       page >= 0 && key < cur.len);
-      }
-    } else {
-#pragma unroll
-      for (int nb = 0; nb < NG; ++nb) {  // 8 keys: two of them are this lane's
-        const int page = __shfl_sync(full, pages, nb), key = key0 + 8 * nb + 2 * t;
-        const uint8_t* row = base + (int64_t)page * (a.cache.ps_p * P::kSize) + (key & row_mask) * row_bytes;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const bool wanted = page >= 0 && key + e < cur.len;
-          if constexpr (P::kRow == 64) {  // e4m3, 64 dimensions: 8 bytes; the lane's keys of a group share a register quadruple
-            const uint2 v = load8(row + e * row_bytes + 8 * g, wanted);
-            (e ? vr[nb].z : vr[nb].x) = v.x;
-            (e ? vr[nb].w : vr[nb].y) = v.y;
-          } else {
-#pragma unroll
-            for (int c = 0; c < P::kRow / 128; ++c)
-              vr[(nb * 2 + e) * (P::kRow / 128) + c] = load16(row + e * row_bytes + 128 * c + 16 * g, wanted);
-          }
-        }
-      }
+    for (int i = 0; i < 8; ++i) {
+      const int row0 = i * kRowsAtOnce, row = row0 + my_row;
+      const int64_t at = __shfl_sync(full, f.at, row0 >> 3);
+      const bool wanted = at >= 0 && row < f.left;
+      fetch16(to + row * P::kRow + (my_piece ^ swizzle(row)) * 16, wanted ? base + at + lane_at + (row0 & 7) * row_bytes : base, wanted);
     }
   };
-  // the lane's part of the query rows of a (sequence, head tile)
-  uint32_t qr[kF32 ? 1 : D / 8], qr8[kF32 || HT == 8 ? 1 : D / 8];
-  float score_scale = 0.f;
+  auto fetch_k = [&](const Place& f) { fetch(f, a.cache.k, queue_at); };
+  auto fetch_v = [&](const Place& f) { fetch(f, a.cache.v, queue_at + 4096); };
+  // 16 bytes of a row of K (of V)
+  auto k_piece = [&](int row, int i) { return *reinterpret_cast<const uint4*>(queue + row * P::kRow + (i ^ swizzle(row)) * 16); };
+  auto v_piece = [&](int row, int i) { return *reinterpret_cast<const uint4*>(queue + 4096 + row * P::kRow + (i ^ swizzle(row)) * 16); };
+
+  // the lane's part of the query rows of a (sequence, head tile): of head g (and g + 8), laid out as the keys are
+  uint32_t qr[kF32 ? 1 : NT][kF32 ? 1 : D / 8];
+  float score_scale[kF16 ? 2 * NT : 1];  // e4m3: of the heads whose scores the lane gets
   auto load_q = [&](const Cursor& cur) {
-    const int kv = cur.hi / a.tiles, h0 = kv * a.group + (cur.hi % a.tiles) * HT, rows = min(HT, (kv + 1) * a.group - h0);
-    score_scale = a.scale_log2e * (kType == kTypeE4m3 && a.cache.k_scale ? a.cache.k_scale[kv] : 1.f);
+    const int kv = cur.hi / a.tiles, h0 = kv * a.group + (cur.hi - kv * a.tiles) * HT, rows = min(HT, (kv + 1) * a.group - h0);
+    const float scale = a.scale_log2e * (kType == kTypeE4m3 && a.cache.k_scale ? a.cache.k_scale[kv] : 1.f);
+    if constexpr (!kF16) score_scale[0] = scale;
     if constexpr (kF32) {
       for (int i = tid; i < HT * D; i += NW * 32)
         q_rows[i / D][i % D] = i / D < rows ? static_cast<const float*>(a.q)[cur.s * a.q_b + (h0 + i / D) * a.q_h + i % D] : 0.f;
     } else {
       constexpr int E = 16 / P::kSize;  // elements of a lane's piece
-      auto load_row = [&](int r, uint32_t* to) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int r = g + 8 * nt;
         const __nv_bfloat16* row = static_cast<const __nv_bfloat16*>(a.q) + cur.s * a.q_b + (int64_t)(h0 + r) * a.q_h;
 #pragma unroll
         for (int c = 0; c < NP; ++c)
@@ -272,185 +295,250 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
             uint4 v = make_uint4(0, 0, 0, 0);
             if (r < rows) v = *reinterpret_cast<const uint4*>(row + c * 4 * E + t * E + e * 8);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) to[(c * (E / 8) + e) * 4 + i] = word(v, i);
+            for (int i = 0; i < 4; ++i) qr[nt][(c * (E / 8) + e) * 4 + i] = word(v, i);
           }
-      };
-      load_row(g, qr);
-      if constexpr (HT == 16) load_row(g + 8, qr8);
+        if constexpr (kF16) {
+          // bf16 -> f16, the row scaled by a power of 2 that puts its largest element at 2^13: exact for elements down to 2^-27 of
+          // that one, and off by 2^-38 of it below
+          float top = 0.f;
+#pragma unroll
+          for (int i = 0; i < D / 8; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(qr[nt][i] << 16)), fabsf(__uint_as_float(qr[nt][i] & 0xffff0000u))));
+          top = fmaxf(top, __shfl_xor_sync(full, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(full, top, 2));
+          const int up = min(max(267 - (int)(__float_as_uint(top) >> 23), 1), 240);  // exponent field of that power
+          const float f = __uint_as_float((uint32_t)up << 23), back = __uint_as_float((uint32_t)(254 - up) << 23);
+#pragma unroll
+          for (int i = 0; i < D / 8; ++i) qr[nt][i] = f16_pair(__uint_as_float(qr[nt][i] << 16) * f, __uint_as_float(qr[nt][i] & 0xffff0000u) * f);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) score_scale[2 * nt + i] = scale * __shfl_sync(full, back, (2 * t + i) * 4);
+        }
+      }
     }
   };
 
   float acc[kAcc][4];
-  float m[HT == 16 && !kF32 ? 2 : 1], l[HT == 16 && !kF32 ? 2 : 1];  // fp32: of row lane % HT, equal in the lanes that share it
+  // heads 8 nt + 2t, + 1: the exponent offset, the same in all lanes that share the heads, and the sum of the lane's own keys' weights;
+  // fp32: of row lane % HT, both equal in the lanes that share it
+  float m[kF32 ? 1 : 2 * NT], l[kF32 ? 1 : 2 * NT];
 
   // ---- the warp's first chunk
+  int x = x0 + warp;        // the chunk in the queue
   Cursor nxt = seg;
   advance(nxt, warp);
-  int64_t x = x0 + warp;  // the chunk in kr and vr
-  int pages = x < x1 ? pages_of(nxt) : -1;
-  if (x < x1) {
-    load_k(nxt, pages);
-    load_v(nxt, pages);
-  }
-  Cursor cur = nxt;
-  advance(nxt, NW);
-  pages = x + NW < x1 ? pages_of(nxt) : -1;
+  int entry = x < x1 ? entry_of(nxt) : -1;
   load_q(seg);
+  Place here{-1, 0};        // of the chunk in the queue
+  if (x < x1) {
+    here = place_of(nxt, entry);
+    fetch_k(here);
+    fetch_commit();
+    fetch_v(here);
+    fetch_commit();
+    advance(nxt, NW);       // the chunk that is fetched next, and the table's entries for it
+    entry = x + NW < x1 ? entry_of(nxt) : -1;
+  }
   if constexpr (kF32) __syncthreads();
 
-  for (int64_t pos = x0; pos < x1;) {
-    const int64_t seg_end = min(x1, seg_first + seg.n);
-    const int kv = seg.hi / a.tiles, h0 = kv * a.group + (seg.hi % a.tiles) * HT, rows = min(HT, (kv + 1) * a.group - h0);
+  for (int pos = x0; pos < x1;) {
+    const int seg_end = min(x1, seg_first + seg.n);
+    const int kv = seg.hi / a.tiles, h0 = kv * a.group + (seg.hi - kv * a.tiles) * HT, rows = min(HT, (kv + 1) * a.group - h0);
 #pragma unroll
     for (int i = 0; i < kAcc; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(m) / 4); ++i) { m[i] = -CUDART_INF_F; l[i] = 0.f; }
 
     for (; x < seg_end; x += NW) {
-      const int left = cur.len - cur.c * KC;  // keys of the chunk that count: 1 and up
-      const bool more_chunks = x + NW < x1;
+      const int left = here.left;  // keys of the chunk that count: 1 and up
+      // two groups of fetches are under way, this chunk's K and its V; further down its V and the next one's K
+      fetch_wait<1>();
+      __syncwarp();
+      const bool next = x + NW < x1;
+      auto k_used = [&] {  // the next chunk's K takes its place
+        __syncwarp();
+        if (next) {
+          here = place_of(nxt, entry);
+          fetch_k(here);
+        }
+        fetch_commit();
+        fetch_wait<1>();
+        __syncwarp();
+      };
+      auto v_used = [&] {
+        __syncwarp();
+        if (next) {
+          fetch_v(here);
+          advance(nxt, NW);
+          entry = x + 2 * NW < x1 ? entry_of(nxt) : -1;
+        }
+        fetch_commit();
+      };
       if constexpr (!kF32) {
-        // ---------------------------------------------------------------- scores
-        float sc[NG][4];
+        // ---------------------------------------------------------------- scores of keys 16 mt + g and + 8, heads 8 nt + 2t and + 1
+        float sc[NG / 2][NT][4];
 #pragma unroll
-        for (int nb = 0; nb < NG; ++nb) {
-          sc[nb][0] = sc[nb][1] = sc[nb][2] = sc[nb][3] = 0.f;
+        for (int mt = 0; mt < NG / 2; ++mt)
 #pragma unroll
-          for (int c = 0; c < NP; ++c) {
-            const uint4 kw = kr[nb * NP + c];
+          for (int nt = 0; nt < NT; ++nt) sc[mt][nt][0] = sc[mt][nt][1] = sc[mt][nt][2] = sc[mt][nt][3] = 0.f;
+#pragma unroll
+        for (int c = 0; c < NP; ++c) {
+#pragma unroll
+          for (int mt = 0; mt < NG / 2; ++mt) {
+            const uint4 k0 = k_piece(16 * mt + g, 4 * c + t), k8 = k_piece(16 * mt + 8 + g, 4 * c + t);
             if constexpr (kType == kTypeBf16) {
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const int w = c * 4 + 2 * e;
-                mma(sc[nb], qr[w], HT == 16 ? qr8[w % (D / 8)] : 0u, qr[w + 1], HT == 16 ? qr8[(w + 1) % (D / 8)] : 0u, word(kw, 2 * e), word(kw, 2 * e + 1));
-              }
+              for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+                  mma<kF16>(sc[mt][nt], word(k0, 2 * e), word(k8, 2 * e), word(k0, 2 * e + 1), word(k8, 2 * e + 1), qr[nt][c * 4 + 2 * e], qr[nt][c * 4 + 2 * e + 1]);
             } else {
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                const int w = c * 8 + 2 * e;
-                mma(sc[nb], qr[w], HT == 16 ? qr8[w] : 0u, qr[w + 1], HT == 16 ? qr8[w + 1] : 0u,
-                    widen_e4m3(__byte_perm(word(kw, e), 0, 0x1100)), widen_e4m3(__byte_perm(word(kw, e), 0, 0x3322)));
+                const uint32_t a0 = widen_lo(word(k0, e)), a1 = widen_lo(word(k8, e)), a2 = widen_hi(word(k0, e)), a3 = widen_hi(word(k8, e));
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma<kF16>(sc[mt][nt], a0, a1, a2, a3, qr[nt][c * 8 + 2 * e], qr[nt][c * 8 + 2 * e + 1]);
               }
             }
           }
         }
-        if (more_chunks) load_k(nxt, pages);
+        k_used();
         // ---------------------------------------------------------------- weights
-        constexpr int NR = HT / 8;
-        float alpha[NR];
+        bool passed = false;
 #pragma unroll
-        for (int r = 0; r < NR; ++r) {
-          float top = -CUDART_INF_F;
+        for (int mt = 0; mt < NG / 2; ++mt)
 #pragma unroll
-          for (int nb = 0; nb < NG; ++nb)
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              float& z = sc[nb][2 * r + e];
-              z = 8 * nb + 2 * t + e < left ? z * score_scale : -CUDART_INF_F;
-              top = fmaxf(top, z);
-            }
-          top = fmaxf(top, __shfl_xor_sync(full, top, 1));
-          top = fmaxf(top, __shfl_xor_sync(full, top, 2));
-          const float m_new = fmaxf(m[r], top);
-          alpha[r] = exp2_approx(m[r] - m_new);
-          m[r] = m_new;
-          float sum = 0.f;
+            for (int e = 0; e < 4; ++e) sc[mt][nt][e] *= score_scale[kF16 ? 2 * nt + (e & 1) : 0];
+        if (left < KC) {
 #pragma unroll
-          for (int nb = 0; nb < NG; ++nb)
+          for (int mt = 0; mt < NG / 2; ++mt)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              float& z = sc[nb][2 * r + e];
-              z = exp2_approx(z - m_new);
-              sum += z;
-            }
-          l[r] = fmaf(l[r], alpha[r], sum);
+            for (int e = 0; e < 4; ++e)
+              if (16 * mt + 8 * (e >> 1) + g >= left) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) sc[mt][nt][e] = -CUDART_INF_F;
+              }
         }
-        bool moved = alpha[0] != 1.f;
-        if (NR == 2) moved |= alpha[NR - 1] != 1.f;
-        if (__any_sync(full, moved)) {
+        float top[2 * NT];
 #pragma unroll
-          for (int i = 0; i < kAcc; ++i) {
-            acc[i][0] *= alpha[0]; acc[i][1] *= alpha[0];
-            acc[i][2] *= alpha[NR - 1]; acc[i][3] *= alpha[NR - 1];
+        for (int i = 0; i < 2 * NT; ++i) {
+          top[i] = -CUDART_INF_F;
+#pragma unroll
+          for (int mt = 0; mt < NG / 2; ++mt) top[i] = fmaxf(top[i], fmaxf(sc[mt][i >> 1][i & 1], sc[mt][i >> 1][2 + (i & 1)]));
+          passed |= top[i] > m[i] + kSlack;
+        }
+        if (__any_sync(full, passed)) {
+#pragma unroll
+          for (int i = 0; i < 2 * NT; ++i) {
+            top[i] = fmaxf(top[i], __shfl_xor_sync(full, top[i], 4));
+            top[i] = fmaxf(top[i], __shfl_xor_sync(full, top[i], 8));
+            top[i] = fmaxf(top[i], __shfl_xor_sync(full, top[i], 16));
+            const float to = fmaxf(m[i], top[i]);
+            const float alpha = m[i] == to ? 1.f : exp2_approx(m[i] - to);
+            m[i] = to;
+            l[i] *= alpha;
+#pragma unroll
+            for (int j = 0; j < kTiles; ++j) {
+              acc[(i >> 1) * kTiles + j][i & 1] *= alpha;
+              acc[(i >> 1) * kTiles + j][2 + (i & 1)] *= alpha;
+            }
           }
         }
+#pragma unroll
+        for (int mt = 0; mt < NG / 2; ++mt)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float& z = sc[mt][nt][e];
+              z = exp2_approx(z - m[2 * nt + (e & 1)]);
+              l[2 * nt + (e & 1)] += z;
+            }
         // ---------------------------------------------------------------- weighted sum of the values
 #pragma unroll
-        for (int sub = 0; sub < NG / 2; ++sub) {
-          float* w0 = sc[2 * sub];
-          float* w1 = sc[2 * sub + 1];
-          const uint32_t a0 = bf16_pair(w0[0], w0[1]), a2 = bf16_pair(w1[0], w1[1]);
-          auto rest = [](uint32_t hi, float x, float y) {  // what the bf16 pair leaves of (x, y)
-            return bf16_pair(x - __uint_as_float(hi << 16), y - __uint_as_float(hi & 0xffff0000u));
-          };
-          const uint32_t r0 = rest(a0, w0[0], w0[1]), r2 = rest(a2, w1[0], w1[1]);
-          uint32_t a1 = r0, a3 = r2, r1 = 0, r3 = 0;
-          if constexpr (HT == 16) {
-            a1 = bf16_pair(w0[2], w0[3]);
-            a3 = bf16_pair(w1[2], w1[3]);
-            r1 = rest(a1, w0[2], w0[3]);
-            r3 = rest(a3, w1[2], w1[3]);
+        for (int mt = 0; mt < NG / 2; ++mt) {
+          uint32_t b0[NT], b1[NT], r0[NT], r1[NT];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            const float(&w)[4] = sc[mt][nt];
+            split_pair<kF16>(w[0], w[1], b0[nt], r0[nt]);
+            split_pair<kF16>(w[2], w[3], b1[nt], r1[nt]);
+            b0[nt] = transposed(b0[nt]);
+            b1[nt] = transposed(b1[nt]);
+            r0[nt] = transposed(r0[nt]);
+            r1[nt] = transposed(r1[nt]);
           }
-          auto step = [&](float (&o)[4], uint32_t b0, uint32_t b1) {
-            mma(o, a0, a1, a2, a3, b0, b1);
-            if constexpr (HT == 16) mma(o, r0, r1, r2, r3, b0, b1);
+          auto step = [&](int j, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              mma<kF16>(acc[nt * kTiles + j], a0, a1, a2, a3, b0[nt], b1[nt]);
+              mma<kF16>(acc[nt * kTiles + j], a0, a1, a2, a3, r0[nt], r1[nt]);
+            }
           };
           if constexpr (kType == kTypeBf16) {
-            constexpr int H2 = D / 64;
+            constexpr int H2 = D / 64;  // pieces of a key
+            uint4 u[4][H2];             // keys 2t, 2t + 1, 2t + 8, 2t + 9
 #pragma unroll
-            for (int h2 = 0; h2 < H2; ++h2) {
-              const uint4 &u0 = vr[(sub * 4 + 0) * H2 + h2], &u1 = vr[(sub * 4 + 1) * H2 + h2], &u2 = vr[(sub * 4 + 2) * H2 + h2],
-                          &u3 = vr[(sub * 4 + 3) * H2 + h2];
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-              for (int j = 0; j < 8; ++j)
-                step(acc[h2 * 8 + j], __byte_perm(word(u0, j >> 1), word(u1, j >> 1), j & 1 ? 0x7632 : 0x5410),
-                     __byte_perm(word(u2, j >> 1), word(u3, j >> 1), j & 1 ? 0x7632 : 0x5410));
+              for (int h = 0; h < H2; ++h) u[i][h] = v_piece(16 * mt + 2 * t + (i & 1) + 8 * (i >> 1), 8 * h + g);
+            auto pair = [&](int i, int h, int j) {  // element j of the piece, of keys i and i + 1
+              return __byte_perm(word(u[i][h], j >> 1), word(u[i + 1][h], j >> 1), j & 1 ? 0x7632 : 0x5410);
+            };
+            // tile j: dimensions 8 g + j and 64 + 8 g + j (64-wide heads: 8 g + j and 8 g + 4 + j)
+#pragma unroll
+            for (int j = 0; j < kTiles; ++j) {
+              if constexpr (D == 128) step(j, pair(0, 0, j), pair(0, H2 - 1, j), pair(2, 0, j), pair(2, H2 - 1, j));
+              else step(j, pair(0, 0, j), pair(0, 0, j + 4), pair(2, 0, j), pair(2, 0, j + 4));
             }
           } else {
-            // byte j of the keys' words into the upper bytes of the halves
-            constexpr uint32_t pick[4] = {0x4400, 0x5511, 0x6622, 0x7733};
+            // a lane's dimensions of a key: 16 bytes, or with 64 dimensions the lower or the upper 8 of them
+            uint32_t u[4][D / 32];
 #pragma unroll
-            for (int j = 0; j < D / 8; ++j) {
-              uint32_t x0w, x1w, x2w, x3w;
-              if constexpr (P::kRow == 64) {
-                const uint4 &u = vr[2 * sub], &v = vr[2 * sub + 1];
-                x0w = word(u, j >> 2); x1w = word(u, 2 + (j >> 2)); x2w = word(v, j >> 2); x3w = word(v, 2 + (j >> 2));
-              } else {
-                x0w = word(vr[sub * 4], j >> 2); x1w = word(vr[sub * 4 + 1], j >> 2);
-                x2w = word(vr[sub * 4 + 2], j >> 2); x3w = word(vr[sub * 4 + 3], j >> 2);
-              }
-              step(acc[j], widen_e4m3(__byte_perm(x0w, x1w, pick[j & 3])), widen_e4m3(__byte_perm(x2w, x3w, pick[j & 3])));
+            for (int i = 0; i < 4; ++i) {
+              const uint4 v = v_piece(16 * mt + 2 * t + (i & 1) + 8 * (i >> 1), D == 64 ? g >> 1 : g);
+#pragma unroll
+              for (int k = 0; k < D / 32; ++k) u[i][k] = D == 64 ? (g & 1 ? word(v, 2 + k) : word(v, k)) : word(v, k);
+            }
+            auto two = [&](int i, int j) {  // bytes j and j + 1 of keys i and i + 1, key by key
+              return __byte_perm(u[i][j >> 2], u[i + 1][j >> 2], j & 2 ? 0x7362 : 0x5140);
+            };
+            // tile j: dimensions 16 g + j and 16 g + 8 + j (64-wide heads: 8 g + j and 8 g + 4 + j)
+#pragma unroll
+            for (int j = 0; j < kTiles; j += 2) {
+              const uint32_t w0 = two(0, j), w1 = two(0, j + kTiles), w2 = two(2, j), w3 = two(2, j + kTiles);
+              step(j, widen_lo(w0), widen_lo(w1), widen_lo(w2), widen_lo(w3));
+              step(j + 1, widen_hi(w0), widen_hi(w1), widen_hi(w2), widen_hi(w3));
             }
           }
         }
-        if (more_chunks) load_v(nxt, pages);
+        v_used();
       } else {
         // ---------------------------------------------------------------- fp32 scores: 4 lanes per key
-        float mine[NG];  // of row lane % HT: keys
 #pragma unroll
-        for (int nb = 0; nb < NG; ++nb) mine[nb] = 0.f;
+        for (int nb = 0; nb < NG; ++nb) {
+          uint4 kr[NP];
 #pragma unroll
-        for (int r = 0; r < HT; ++r) {
-          if (r < rows) {
+          for (int c = 0; c < NP; ++c) kr[c] = k_piece(8 * nb + g, 4 * c + t);
 #pragma unroll
-            for (int nb = 0; nb < NG; ++nb) {
+          for (int r = 0; r < HT; ++r) {
+            if (r < rows) {
               float z = 0.f;
 #pragma unroll
               for (int c = 0; c < NP; ++c) {
                 const float4 qv = *reinterpret_cast<const float4*>(&q_rows[r][16 * c + 4 * t]);
-                const uint4 kw = kr[nb * NP + c];
-                z = fmaf(qv.x, __uint_as_float(kw.x), z);
-                z = fmaf(qv.y, __uint_as_float(kw.y), z);
-                z = fmaf(qv.z, __uint_as_float(kw.z), z);
-                z = fmaf(qv.w, __uint_as_float(kw.w), z);
+                z = fmaf(qv.x, __uint_as_float(kr[c].x), z);
+                z = fmaf(qv.y, __uint_as_float(kr[c].y), z);
+                z = fmaf(qv.z, __uint_as_float(kr[c].z), z);
+                z = fmaf(qv.w, __uint_as_float(kr[c].w), z);
               }
               z += __shfl_xor_sync(full, z, 1);
               z += __shfl_xor_sync(full, z, 2);
-              if (t == 0) weights[warp][8 * nb + g][r] = 8 * nb + g < left ? z * score_scale : -CUDART_INF_F;
+              if (t == 0) weights[warp][8 * nb + g][r] = 8 * nb + g < left ? z * score_scale[0] : -CUDART_INF_F;
             }
           }
         }
-        if (more_chunks) load_k(nxt, pages);
+        k_used();
         __syncwarp();
         // row lane % HT, keys lane / HT, + 32 / HT, ...
         {
@@ -462,33 +550,35 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
             z[i] = r < rows ? weights[warp][i * KL + lane / HT][r] : 0.f;
             top = fmaxf(top, z[i]);
           }
+          if (__any_sync(full, top > m[0] + kSlack)) {
 #pragma unroll
-          for (int off = HT; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(full, top, off));
-          const float m_new = fmaxf(m[0], top), alpha = exp2f(m[0] - m_new);
-          m[0] = m_new;
-          float sum = 0.f;
-#pragma unroll
-          for (int i = 0; i < KC / KL; ++i) {
-            z[i] = exp2f(z[i] - m_new);
-            sum += z[i];
-            weights[warp][i * KL + lane / HT][r] = z[i];
-          }
-#pragma unroll
-          for (int off = HT; off < 32; off <<= 1) sum += __shfl_xor_sync(full, sum, off);
-          l[0] = fmaf(l[0], alpha, sum);
-          if (__any_sync(full, alpha != 1.f)) {
+            for (int off = HT; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(full, top, off));
+            const float to = fmaxf(m[0], top), alpha = m[0] == to ? 1.f : exp2f(m[0] - to);
+            m[0] = to;
+            l[0] *= alpha;
 #pragma unroll
             for (int i = 0; i < HT; ++i) {
               const float f = __shfl_sync(full, alpha, i);
               acc[i][0] *= f; acc[i][1] *= f; acc[i][2] *= f; acc[i][3] *= f;
             }
           }
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < KC / KL; ++i) {
+            z[i] = exp2f(z[i] - m[0]);
+            sum += z[i];
+            weights[warp][i * KL + lane / HT][r] = z[i];
+          }
+#pragma unroll
+          for (int off = HT; off < 32; off <<= 1) sum += __shfl_xor_sync(full, sum, off);
+          l[0] += sum;
         }
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int in = D == 128 ? i : 2 * i + (lane >> 4);
-          const float4 v = make_float4(__uint_as_float(vr[i].x), __uint_as_float(vr[i].y), __uint_as_float(vr[i].z), __uint_as_float(vr[i].w));
+          const uint4 vw = v_piece(in, D == 128 ? lane : lane & 15);
+          const float4 v = make_float4(__uint_as_float(vw.x), __uint_as_float(vw.y), __uint_as_float(vw.z), __uint_as_float(vw.w));
 #pragma unroll
           for (int r4 = 0; r4 < HT / 4; ++r4) {
             if (r4 * 4 < rows) {
@@ -505,26 +595,22 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
             }
           }
         }
-        if (more_chunks) load_v(nxt, pages);
+        v_used();
         __syncwarp();
       }
-      cur = nxt;
-      advance(nxt, NW);
-      pages = x + 2 * NW < x1 ? pages_of(nxt) : -1;
     }
 
     // ---- the stretch ends: what the warps hold meets in shared memory, 8 rows at a time
     const Cursor done = seg;
-    const int64_t done_first = seg_first;
-    advance(seg, (int)(seg_end - pos));  // the next stretch; its queries are requested before the barriers below
-    seg_first = seg_end;                 // (a stretch that does not end its sequence is the block's last)
+    const int done_first = seg_first;
+    advance(seg, seg_end - pos);  // the next stretch; its queries are requested before the barriers below
+    seg_first = seg_end;          // (a stretch that does not end its sequence is the block's last)
     if constexpr (!kF32)
       if (seg_end < x1) load_q(seg);
     const bool whole = done_first >= x0 && done_first + done.n <= x1;
     const bool begins_before = done_first < x0;
-    const int64_t b_first = whole ? 0 : block_of(done_first);
     const float v_scale = kType == kTypeE4m3 && a.cache.v_scale ? a.cache.v_scale[kv] : 1.f;
-    float* slot = a.parts + (2 * (int64_t)blockIdx.x + (begins_before ? 1 : 0)) * P::kSlot;
+    float* slot = a.parts + (2 * (int)blockIdx.x + (begins_before ? 1 : 0)) * P::kSlot;
 
     // rows [8 half, 8 half + 8) of all warps -> the sequence's output, or the block's part in the workspace
     auto meet = [&](int half, bool final) {
@@ -536,7 +622,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
         for (int w = 1; w < NW; ++w) top = fmaxf(top, part_m[w][r]);
         float sum = 0.f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
+#pragma unroll 4
         for (int w = 0; w < NW; ++w) {
           const float mw = part_m[w][r];
           if (mw == -CUDART_INF_F) continue;  // a warp without a chunk
@@ -560,7 +646,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
       __syncthreads();
     };
 #pragma unroll
-    for (int half = 0; half < HT / 8; ++half) {
+    for (int half = 0; half < NT; ++half) {
       if (8 * half >= rows) break;
       if constexpr (kF32) {
 #pragma unroll
@@ -574,46 +660,45 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
         }
         if (lane >= 8 * half && lane < 8 * half + 8) { part_m[warp][lane - 8 * half] = m[0]; part_l[warp][lane - 8 * half] = l[0]; }
       } else {
-        float sum = l[HT == 16 ? half : 0];
-        sum += __shfl_xor_sync(full, sum, 1);
-        sum += __shfl_xor_sync(full, sum, 2);
-        if (t == 0) { part_m[warp][g] = m[HT == 16 ? half : 0]; part_l[warp][g] = sum; }
-        if (8 * half + g < rows) {
-          constexpr int kRun = P::kSize == 1 && D == 128 ? 16 : 8;  // columns of a lane in a row, per run
 #pragma unroll
-          for (int i = 0; i < kAcc / kRun; ++i)
+        for (int i = 0; i < 2; ++i) {
+          float sum = l[2 * half + i];
+          sum += __shfl_xor_sync(full, sum, 4);
+          sum += __shfl_xor_sync(full, sum, 8);
+          sum += __shfl_xor_sync(full, sum, 16);
+          if (g == 0) { part_m[warp][2 * t + i] = m[2 * half + i]; part_l[warp][2 * t + i] = sum; }
+          if (8 * half + 2 * t + i < rows) {
+            constexpr bool kSplitRuns = kType == kTypeBf16 && D == 128;  // where the tiles' second dimensions lie
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
+            for (int run = 0; run < 2; ++run)
 #pragma unroll
-              for (int j = 0; j < kRun; j += 4) {
+              for (int j = 0; j < kTiles; j += 4) {
                 float v[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                  const float(&o)[4] = acc[i * kRun + j + k];
-                  v[k] = HT == 16 ? o[2 * half + e] : o[e] + o[2 + e];
-                }
-                *reinterpret_cast<float4*>(&part_o[warp][g][i * 64 + (2 * t + e) * kRun + j]) = make_float4(v[0], v[1], v[2], v[3]);
+                for (int k = 0; k < 4; ++k) v[k] = acc[half * kTiles + j + k][2 * run + i];
+                const int col = (kSplitRuns ? 64 * run + 8 * g : (2 * g + run) * kTiles) + j;
+                *reinterpret_cast<float4*>(&part_o[warp][2 * t + i][col]) = make_float4(v[0], v[1], v[2], v[3]);
               }
+          }
         }
       }
       meet(half, whole);
     }
     if (!whole) {
-      // The part is in the workspace.  The last of the sequence's blocks to arrive puts all parts together.
-      const int64_t b_last = block_of(done_first + done.n - 1);
-      const int n_parts = (int)(b_last - b_first) + 1;
-      __threadfence();
-      __syncthreads();
+      // The part is in the workspace.  The last of the sequence's blocks to arrive puts all parts together.  (The barrier at the end of meet() puts
+      // the block's writes before the arrival, whose release and acquire take them to the block that arrives last.)
+      const int b_first = block_of(done_first), n_parts = block_of(done_first + done.n - 1) - b_first + 1;
       if (tid == 0) {
-        last_arrival = atomicAdd(a.tickets + b_first, 1u) + 1u == (unsigned)n_parts;
+        unsigned before;
+        asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.tickets + b_first) : "memory");
+        last_arrival = before + 1 == (unsigned)n_parts;
         if (last_arrival) a.tickets[b_first] = 0;
-        __threadfence();
       }
       __syncthreads();
       if (last_arrival) {
         auto part_at = [&](int i) { return a.parts + (2 * (b_first + i) + (i ? 1 : 0)) * P::kSlot; };
 #pragma unroll 1
-        for (int half = 0; half < HT / 8; ++half) {
+        for (int half = 0; half < NT; ++half) {
           if (8 * half >= rows) break;
           // this warp's parts: warp, warp + NW, ...; lane = (part in a group of 4, row)
           constexpr int kRounds = (kTokenBlocks + 4 * NW - 1) / (4 * NW);
@@ -641,21 +726,21 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
           constexpr int kVec = 8 * D / 128;  // float4 of the 8 rows, per lane
 #pragma unroll
           for (int v = 0; v < kVec; ++v) {
-            const int e = lane + 32 * v, vr_ = e / (D / 4), col = 4 * (e % (D / 4));
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            const int e = lane + 32 * v, row = e / (D / 4), col = 4 * (e % (D / 4));
             if (8 * half + (32 * v) / (D / 4) >= rows) break;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int k = 0; k < kRounds; ++k)
 #pragma unroll
               for (int q = 0; q < 4; ++q) {
                 const int i = warp + NW * (4 * k + q);
-                const float f = __shfl_sync(full, pm[k], q * 8 + vr_);
-                if (i < n_parts && 8 * half + vr_ < rows) {
-                  const float4 x4 = __ldcg(reinterpret_cast<const float4*>(part_at(i) + (8 * half + vr_) * D + col));
+                const float f = __shfl_sync(full, pm[k], q * 8 + row);
+                if (i < n_parts && 8 * half + row < rows) {
+                  const float4 x4 = __ldcg(reinterpret_cast<const float4*>(part_at(i) + (8 * half + row) * D + col));
                   o.x = fmaf(x4.x, f, o.x); o.y = fmaf(x4.y, f, o.y); o.z = fmaf(x4.z, f, o.z); o.w = fmaf(x4.w, f, o.w);
                 }
               }
-            *reinterpret_cast<float4*>(&part_o[warp][vr_][col]) = o;
+            *reinterpret_cast<float4*>(&part_o[warp][row][col]) = o;
           }
           meet(half, true);
         }
@@ -675,12 +760,32 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
 // Heads per tile: 8 where they suffice (the residuals then ride in the other 8 rows of a product).
 static int head_tile(int group) { return group <= 8 ? 8 : 16; }
 
+// The kernel's dynamic shared memory limit, an attribute per device.
+template <int D, int kType, int HT>
+static cudaError_t allow_smem() {
+  constexpr int kMaxDevices = 64;
+  static std::mutex mu;
+  static bool done[kMaxDevices];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+  std::lock_guard<std::mutex> lock(mu);
+  if (done[dev]) return cudaSuccess;
+  e = cudaFuncSetAttribute(paged_attention_kernel<D, kType, HT>, cudaFuncAttributeMaxDynamicSharedMemorySize, TokenPlan<D, kType, HT>::kBytes);
+  done[dev] = e == cudaSuccess;
+  return e;
+}
+
 template <int D, int kType, int HT>
 static int launch_token(const TokenParams& p, cudaStream_t stream) {
   using P = TokenPlan<D, kType, HT>;
   const int64_t most = (int64_t)p.S * p.Hkv * p.tiles * ((p.cache.cap + P::kKeys - 1) / P::kKeys);  // chunks, if every sequence were full
-  const int64_t grid = std::min<int64_t>(kTokenBlocks, (most + P::kWarps * kMinRounds - 1) / (P::kWarps * kMinRounds));
-  const cudaError_t e = launch(paged_attention_kernel<D, kType, HT>, dim3((unsigned)std::max<int64_t>(grid, 1)), dim3(P::kWarps * 32), 0, stream, p);
+  if (most >= (1 << 30)) return TSD_ERR_UNSUPPORTED;
+  const int64_t grid = std::min<int64_t>(kTokenBlocks, (most + P::kWarps - 1) / P::kWarps);
+  cudaError_t e = allow_smem<D, kType, HT>();
+  if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(paged_attention_kernel)");
+  e = launch(paged_attention_kernel<D, kType, HT>, dim3((unsigned)std::max<int64_t>(grid, 1)), dim3(P::kWarps * 32), P::kBytes, stream, p);
   return e != cudaSuccess ? cuda_fail(e, "paged_attention_kernel") : TSD_OK;
 }
 
