@@ -28,6 +28,7 @@
 namespace tsd {
 
 constexpr int kTokenBlocks = kPlanSms;  // at most: what the workspace is sized for
+constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;           // by how much a score may pass the offset, as a power of 2
 
 enum { kTypeF32 = TSD_F32, kTypeBf16 = TSD_BF16, kTypeE4m3 = TSD_E4M3 };
@@ -41,10 +42,10 @@ struct TokenPlan {
   static constexpr int kGroups = 8 / kPieces;                                  // groups of 8 keys per chunk
   static constexpr int kKeys = 8 * kGroups;                                    // keys per chunk
   static constexpr int kSlot = HT * D + 2 * HT;                                // floats of a part in the workspace
-  static constexpr int kPitch = D + 4;                                         // floats between rows in shared memory
-  // dynamic shared memory: the warps' queues (a chunk's K, its V), then the warps' parts
+  // dynamic shared memory: the warps' queues (a chunk's K, its V), then a part of each warp
   static constexpr int kQueue = kWarps * 8192;
-  static constexpr int kBytes = kQueue + kWarps * 8 * kPitch * 4;
+  static constexpr int kPart = HT * D;                                         // floats: at most a warp's queue
+  static constexpr int kBytes = kQueue + kWarps * kPart * 4;
 };
 
 struct TokenParams {
@@ -134,13 +135,17 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   constexpr int NW = P::kWarps, KC = P::kKeys, NG = P::kGroups, NP = P::kPieces, NT = HT / 8;
   constexpr bool kF32 = kType == kTypeF32, kF16 = kType == kTypeE4m3;  // e4m3 is a subset of f16
   constexpr int kTiles = D / 16;                       // of 16 dimensions
+  constexpr bool kSplitRuns = kType == kTypeBf16 && D == 128;  // where the tiles' second dimensions lie
   constexpr int kAcc = kF32 ? HT : kTiles * NT;        // rows of 4 dimensions (fp32), or tiles of 16 dimensions x 8 heads
   extern __shared__ __align__(16) uint8_t dynamic[];
-  float (*part_o)[8][P::kPitch] = reinterpret_cast<float (*)[8][P::kPitch]>(dynamic + P::kQueue);
-  __shared__ float part_m[NW][8], part_l[NW][8];
+  // Parts of the block's warps, two of each: of a sequence that begins before the warp's stretch (in shared memory of its own), and of one that
+  // goes on behind it (in the warp's queue, which is empty by then).  A sequence here is one of a head tile.
+  auto part_of = [&](int i) { return reinterpret_cast<float*>(i & 1 ? dynamic + (i >> 1) * 8192 : dynamic + P::kQueue + (i >> 1) * P::kPart * 4); };
+  __shared__ float part_m[2 * NW][HT], part_l[2 * NW][HT];
+  __shared__ int part_s[2 * NW], part_hi[2 * NW], part_first[2 * NW], part_n[2 * NW];  // whose: first chunk, chunks (0: no part)
   __shared__ __align__(16) float weights[kF32 ? NW : 1][kF32 ? KC : 1][HT];
-  __shared__ __align__(16) float q_rows[kF32 ? HT : 1][kF32 ? D : 1];
   __shared__ int last_arrival;
+  static_assert(2 * NW <= 32, "a lane per part");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   constexpr unsigned full = 0xffffffffu;
   TokenParams a = p;
@@ -173,14 +178,15 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   auto first_of = [&](int b) { return b * each + min(b, more); };
   auto block_of = [&](int x) { return x < more * (each + 1) ? x / (each + 1) : more + (x - more * (each + 1)) / each; };
   const int x0 = first_of(blockIdx.x), x1 = first_of(blockIdx.x + 1);
+  // and its warps an even share of that, [w0, w1) for this one
+  const int w0 = x0 + warp * ((x1 - x0) / NW) + min(warp, (x1 - x0) % NW), w1 = w0 + (x1 - x0) / NW + (warp < (x1 - x0) % NW ? 1 : 0);
 
-  // ---- where chunk x0 lies
-  Cursor seg;     // of the block's stretch at hand
-  int seg_first;  // first chunk of its (sequence, head tile)
+  // ---- where chunk w0 lies
+  Cursor cur;
   {
     int before = 0;
-    seg.s = 0;
-    seg.len = 0;
+    cur.s = 0;
+    cur.len = 0;
     for (int s0 = 0; s0 < a.S; s0 += 32) {
       const int len = s0 == 0 ? len0 : s0 + lane < a.S ? length(s0 + lane) : 0;
       const int mine = chunks(len) * HI;
@@ -190,38 +196,35 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
         const int o = __shfl_up_sync(full, upto, off);
         if (lane >= off) upto += o;
       }
-      const unsigned hit = __ballot_sync(full, before + upto > x0);
+      const unsigned hit = __ballot_sync(full, before + upto > w0);
       if (hit) {
         const int l = __ffs(hit) - 1;
-        seg.s = s0 + l;
-        seg.len = __shfl_sync(full, len, l);
+        cur.s = s0 + l;
+        cur.len = __shfl_sync(full, len, l);
         before += __shfl_sync(full, upto - mine, l);
         break;
       }
       before += __shfl_sync(full, upto, 31);
     }
-    seg.n = chunks(seg.len);
-    seg.hi = (x0 - before) / seg.n;
-    seg.c = (x0 - before) - seg.hi * seg.n;
-    seg_first = x0 - seg.c;
+    cur.n = max(chunks(cur.len), 1);
+    cur.hi = (w0 - before) / cur.n;
+    cur.c = (w0 - before) - cur.hi * cur.n;
   }
-  auto advance = [&](Cursor& cur, int step) {
-    cur.c += step;
-    while (cur.c >= cur.n) {
-      cur.c -= cur.n;
-      if (++cur.hi == HI) {
-        cur.hi = 0;
-        do {
-          if (++cur.s >= a.S) {  // behind the last chunk: never fetched
-            cur.n = 0x7fffffff;
-            cur.len = 0;
-            break;
-          }
-          cur.len = length(cur.s);
-          cur.n = chunks(cur.len);
-        } while (cur.n == 0);
+  // to the next chunk
+  auto advance = [&](Cursor& c) {
+    if (++c.c < c.n) return;
+    c.c = 0;
+    if (++c.hi < HI) return;
+    c.hi = 0;
+    do {
+      if (++c.s >= a.S) {  // behind the last chunk: never fetched
+        c.n = 0x7fffffff;
+        c.len = 0;
+        return;
       }
-    }
+      c.len = length(c.s);
+      c.n = chunks(c.len);
+    } while (c.n == 0);
   };
 
   const int row_mask = (1 << a.cache.shift) - 1;
@@ -272,46 +275,52 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   auto k_piece = [&](int row, int i) { return *reinterpret_cast<const uint4*>(queue + row * P::kRow + (i ^ swizzle(row)) * 16); };
   auto v_piece = [&](int row, int i) { return *reinterpret_cast<const uint4*>(queue + 4096 + row * P::kRow + (i ^ swizzle(row)) * 16); };
 
-  // the lane's part of the query rows of a (sequence, head tile): of head g (and g + 8), laid out as the keys are
+  // A head tile's heads: the first one, how many.
+  auto first_head = [&](int hi) { return hi / a.tiles * a.group + hi % a.tiles * HT; };
+  auto heads_of = [&](int hi) { return min(HT, a.group - hi % a.tiles * HT); };
+  // the lane's part of the query rows of a (sequence, head tile): of head g (and g + 8), laid out as the keys are; fp32 reads them where they are
   uint32_t qr[kF32 ? 1 : NT][kF32 ? 1 : D / 8];
   float score_scale[kF16 ? 2 * NT : 1];  // e4m3: of the heads whose scores the lane gets
-  auto load_q = [&](const Cursor& cur) {
-    const int kv = cur.hi / a.tiles, h0 = kv * a.group + (cur.hi - kv * a.tiles) * HT, rows = min(HT, (kv + 1) * a.group - h0);
-    const float scale = a.scale_log2e * (kType == kTypeE4m3 && a.cache.k_scale ? a.cache.k_scale[kv] : 1.f);
-    if constexpr (!kF16) score_scale[0] = scale;
-    if constexpr (kF32) {
-      for (int i = tid; i < HT * D; i += NW * 32)
-        q_rows[i / D][i % D] = i / D < rows ? static_cast<const float*>(a.q)[cur.s * a.q_b + (h0 + i / D) * a.q_h + i % D] : 0.f;
-    } else {
+  auto load_q = [&](const Cursor& c) {
+    if constexpr (!kF32) {
       constexpr int E = 16 / P::kSize;  // elements of a lane's piece
+      const int h0 = first_head(c.hi), rows = heads_of(c.hi);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int r = g + 8 * nt;
-        const __nv_bfloat16* row = static_cast<const __nv_bfloat16*>(a.q) + cur.s * a.q_b + (int64_t)(h0 + r) * a.q_h;
+        const __nv_bfloat16* row = static_cast<const __nv_bfloat16*>(a.q) + c.s * a.q_b + (int64_t)(h0 + r) * a.q_h;
 #pragma unroll
-        for (int c = 0; c < NP; ++c)
+        for (int pc = 0; pc < NP; ++pc)
 #pragma unroll
           for (int e = 0; e < E / 8; ++e) {
             uint4 v = make_uint4(0, 0, 0, 0);
-            if (r < rows) v = *reinterpret_cast<const uint4*>(row + c * 4 * E + t * E + e * 8);
+            if (r < rows) v = *reinterpret_cast<const uint4*>(row + pc * 4 * E + t * E + e * 8);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) qr[nt][(c * (E / 8) + e) * 4 + i] = word(v, i);
+            for (int i = 0; i < 4; ++i) qr[nt][(pc * (E / 8) + e) * 4 + i] = word(v, i);
           }
-        if constexpr (kF16) {
-          // bf16 -> f16, the row scaled by a power of 2 that puts its largest element at 2^13: exact for elements down to 2^-27 of
-          // that one, and off by 2^-38 of it below
-          float top = 0.f;
+      }
+    }
+  };
+  auto take_q = [&](const Cursor& c) {
+    const float scale = a.scale_log2e * (kF16 && a.cache.k_scale ? a.cache.k_scale[c.hi / a.tiles] : 1.f);
+    if constexpr (!kF16) {
+      score_scale[0] = scale;
+    } else {
+      // bf16 -> f16, the row scaled by a power of 2 that puts its largest element at 2^13: exact for elements down to 2^-27 of
+      // that one, and off by 2^-38 of it below
 #pragma unroll
-          for (int i = 0; i < D / 8; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(qr[nt][i] << 16)), fabsf(__uint_as_float(qr[nt][i] & 0xffff0000u))));
-          top = fmaxf(top, __shfl_xor_sync(full, top, 1));
-          top = fmaxf(top, __shfl_xor_sync(full, top, 2));
-          const int up = min(max(267 - (int)(__float_as_uint(top) >> 23), 1), 240);  // exponent field of that power
-          const float f = __uint_as_float((uint32_t)up << 23), back = __uint_as_float((uint32_t)(254 - up) << 23);
+      for (int nt = 0; nt < NT; ++nt) {
+        float top = 0.f;
 #pragma unroll
-          for (int i = 0; i < D / 8; ++i) qr[nt][i] = f16_pair(__uint_as_float(qr[nt][i] << 16) * f, __uint_as_float(qr[nt][i] & 0xffff0000u) * f);
+        for (int i = 0; i < D / 8; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(qr[nt][i] << 16)), fabsf(__uint_as_float(qr[nt][i] & 0xffff0000u))));
+        top = fmaxf(top, __shfl_xor_sync(full, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(full, top, 2));
+        const int up = min(max(267 - (int)(__float_as_uint(top) >> 23), 1), 240);  // exponent field of that power
+        const float f = __uint_as_float((uint32_t)up << 23), back = __uint_as_float((uint32_t)(254 - up) << 23);
 #pragma unroll
-          for (int i = 0; i < 2; ++i) score_scale[2 * nt + i] = scale * __shfl_sync(full, back, (2 * t + i) * 4);
-        }
+        for (int i = 0; i < D / 8; ++i) qr[nt][i] = f16_pair(__uint_as_float(qr[nt][i] << 16) * f, __uint_as_float(qr[nt][i] & 0xffff0000u) * f);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) score_scale[2 * nt + i] = scale * __shfl_sync(full, back, (2 * t + i) * 4);
       }
     }
   };
@@ -321,43 +330,109 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   // fp32: of row lane % HT, both equal in the lanes that share it
   float m[kF32 ? 1 : 2 * NT], l[kF32 ? 1 : 2 * NT];
 
-  // ---- the warp's first chunk
-  int x = x0 + warp;        // the chunk in the queue
-  Cursor nxt = seg;
-  advance(nxt, warp);
-  int entry = x < x1 ? entry_of(nxt) : -1;
-  load_q(seg);
-  Place here{-1, 0};        // of the chunk in the queue
-  if (x < x1) {
-    here = place_of(nxt, entry);
-    fetch_k(here);
-    fetch_commit();
-    fetch_v(here);
-    fetch_commit();
-    advance(nxt, NW);       // the chunk that is fetched next, and the table's entries for it
-    entry = x + NW < x1 ? entry_of(nxt) : -1;
-  }
-  if constexpr (kF32) __syncthreads();
-
-  for (int pos = x0; pos < x1;) {
-    const int seg_end = min(x1, seg_first + seg.n);
-    const int kv = seg.hi / a.tiles, h0 = kv * a.group + (seg.hi - kv * a.tiles) * HT, rows = min(HT, (kv + 1) * a.group - h0);
+  auto clear = [&] {
 #pragma unroll
     for (int i = 0; i < kAcc; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(m) / 4); ++i) { m[i] = -CUDART_INF_F; l[i] = 0.f; }
+  };
+  // What a sequence's chunks have come to so far: put aside as part i of the block, or, if they are all of it, written out.
+  auto put_aside = [&](const Cursor& c, int first, int i) {
+    float* o = part_of(i);
+    const int rows = heads_of(c.hi);
+    if (lane == 0) { part_s[i] = c.s; part_hi[i] = c.hi; part_first[i] = first; part_n[i] = c.n; }
+    if constexpr (kF32) {
+#pragma unroll
+      for (int r = 0; r < HT; ++r)
+        if (r < rows && (D == 128 || lane < 16)) *reinterpret_cast<float4*>(o + r * D + 4 * lane) = make_float4(acc[r][0], acc[r][1], acc[r][2], acc[r][3]);
+      if (lane < HT) { part_m[i][lane] = m[0]; part_l[i][lane] = l[0]; }
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2 * NT; ++h) {
+        const int head = 8 * (h >> 1) + 2 * t + (h & 1);
+        if (g == 0) { part_m[i][head] = m[h]; part_l[i][head] = l[h]; }
+        if (head < rows) {
+#pragma unroll
+          for (int run = 0; run < 2; ++run)
+#pragma unroll
+            for (int j = 0; j < kTiles; j += 4) {
+              float v[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) v[k] = acc[(h >> 1) * kTiles + j + k][2 * run + (h & 1)];
+              *reinterpret_cast<float4*>(o + head * D + (kSplitRuns ? 64 * run + 8 * g : (2 * g + run) * kTiles) + j) = make_float4(v[0], v[1], v[2], v[3]);
+            }
+        }
+      }
+    }
+  };
+  auto write_out = [&](const Cursor& c) {
+    const int h0 = first_head(c.hi), rows = heads_of(c.hi);
+    const float v_scale = kF16 && a.cache.v_scale ? a.cache.v_scale[c.hi / a.tiles] : 1.f;
+    const int64_t to = c.s * a.o_b + (int64_t)h0 * a.o_h, lse_to = (int64_t)c.s * a.Hq + h0;
+    if constexpr (kF32) {
+#pragma unroll
+      for (int r = 0; r < HT; ++r) {
+        const float f = 1.f / __shfl_sync(full, l[0], r);
+        if (r < rows && (D == 128 || lane < 16))
+          *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to + r * a.o_h + 4 * lane) = make_float4(acc[r][0] * f, acc[r][1] * f, acc[r][2] * f, acc[r][3] * f);
+      }
+      if (a.lse && lane < rows) a.lse[lse_to + lane] = (m[0] + log2f(l[0])) * kLn2;
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2 * NT; ++h) {
+        const int head = 8 * (h >> 1) + 2 * t + (h & 1);
+        if (head < rows) {
+          const float f = v_scale / l[h];
+          __nv_bfloat16* row = static_cast<__nv_bfloat16*>(a.out) + to + head * a.o_h;
+#pragma unroll
+          for (int run = 0; run < 2; ++run) {
+            uint32_t w[kTiles / 2];
+#pragma unroll
+            for (int j = 0; j < kTiles / 2; ++j)
+              w[j] = bf16_pair(acc[(h >> 1) * kTiles + 2 * j][2 * run + (h & 1)] * f, acc[(h >> 1) * kTiles + 2 * j + 1][2 * run + (h & 1)] * f);
+            __nv_bfloat16* at = row + (kSplitRuns ? 64 * run + 8 * g : (2 * g + run) * kTiles);
+            if constexpr (kTiles == 8) *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+            else *reinterpret_cast<uint2*>(at) = make_uint2(w[0], w[1]);
+          }
+          if (a.lse && g == 0) a.lse[lse_to + head] = (m[h] + log2f(l[h])) * kLn2;
+        }
+      }
+    }
+  };
 
-    for (; x < seg_end; x += NW) {
+  // ---- the warp's first chunk
+  if (lane < 2) part_n[2 * warp + lane] = 0;
+  Place here{-1, 0};        // of the chunk in the queue
+  int entry = -1;           // the table's entries for the chunk that is fetched next
+  if (w0 < w1) {
+    here = place_of(cur, entry_of(cur));
+    fetch_k(here);
+    fetch_commit();
+    fetch_v(here);
+    fetch_commit();
+    load_q(cur);
+    Cursor next = cur;
+    advance(next);
+    if (w0 + 1 < w1) entry = entry_of(next);
+    take_q(cur);
+  }
+  clear();
+  {
+    for (int x = w0; x < w1; ++x) {
       const int left = here.left;  // keys of the chunk that count: 1 and up
+      const int rows = heads_of(cur.hi);
       // two groups of fetches are under way, this chunk's K and its V; further down its V and the next one's K
       fetch_wait<1>();
       __syncwarp();
-      const bool next = x + NW < x1;
+      const bool more_chunks = x + 1 < w1, ends = cur.c + 1 == cur.n;  // of the warp; the sequence
+      Cursor next = cur;
       auto k_used = [&] {  // the next chunk's K takes its place
         __syncwarp();
-        if (next) {
-          here = place_of(nxt, entry);
+        advance(next);
+        if (more_chunks) {
+          here = place_of(next, entry);
           fetch_k(here);
+          if (ends) load_q(next);
         }
         fetch_commit();
         fetch_wait<1>();
@@ -365,10 +440,11 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
       };
       auto v_used = [&] {
         __syncwarp();
-        if (next) {
+        if (more_chunks) {
           fetch_v(here);
-          advance(nxt, NW);
-          entry = x + 2 * NW < x1 ? entry_of(nxt) : -1;
+          Cursor then = next;
+          advance(then);
+          if (x + 2 < w1) entry = entry_of(then);
         }
         fetch_commit();
       };
@@ -515,6 +591,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
         v_used();
       } else {
         // ---------------------------------------------------------------- fp32 scores: 4 lanes per key
+        const float* q32 = static_cast<const float*>(a.q) + cur.s * a.q_b + (int64_t)first_head(cur.hi) * a.q_h;
 #pragma unroll
         for (int nb = 0; nb < NG; ++nb) {
           uint4 kr[NP];
@@ -526,7 +603,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
               float z = 0.f;
 #pragma unroll
               for (int c = 0; c < NP; ++c) {
-                const float4 qv = *reinterpret_cast<const float4*>(&q_rows[r][16 * c + 4 * t]);
+                const float4 qv = __ldg(reinterpret_cast<const float4*>(q32 + r * a.q_h + 16 * c + 4 * t));
                 z = fmaf(qv.x, __uint_as_float(kr[c].x), z);
                 z = fmaf(qv.y, __uint_as_float(kr[c].y), z);
                 z = fmaf(qv.z, __uint_as_float(kr[c].z), z);
@@ -598,161 +675,167 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
         v_used();
         __syncwarp();
       }
-    }
-
-    // ---- the stretch ends: what the warps hold meets in shared memory, 8 rows at a time
-    const Cursor done = seg;
-    const int done_first = seg_first;
-    advance(seg, seg_end - pos);  // the next stretch; its queries are requested before the barriers below
-    seg_first = seg_end;          // (a stretch that does not end its sequence is the block's last)
-    if constexpr (!kF32)
-      if (seg_end < x1) load_q(seg);
-    const bool whole = done_first >= x0 && done_first + done.n <= x1;
-    const bool begins_before = done_first < x0;
-    const float v_scale = kType == kTypeE4m3 && a.cache.v_scale ? a.cache.v_scale[kv] : 1.f;
-    float* slot = a.parts + (2 * (int)blockIdx.x + (begins_before ? 1 : 0)) * P::kSlot;
-
-    // rows [8 half, 8 half + 8) of all warps -> the sequence's output, or the block's part in the workspace
-    auto meet = [&](int half, bool final) {
-      __syncthreads();
-      for (int e = tid; e < min(8, rows - 8 * half) * (D / 4); e += NW * 32) {
-        const int r = e / (D / 4), col = 4 * (e % (D / 4));
-        float top = part_m[0][r];
-#pragma unroll
-        for (int w = 1; w < NW; ++w) top = fmaxf(top, part_m[w][r]);
-        float sum = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int w = 0; w < NW; ++w) {
-          const float mw = part_m[w][r];
-          if (mw == -CUDART_INF_F) continue;  // a warp without a chunk
-          const float f = exp2f(mw - top);
-          const float4 v = *reinterpret_cast<const float4*>(&part_o[w][r][col]);
-          sum = fmaf(part_l[w][r], f, sum);
-          o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
-        }
-        const int row = 8 * half + r;
-        if (final) {
-          const float f = v_scale / sum;
-          const int64_t to = done.s * a.o_b + (int64_t)(h0 + row) * a.o_h + col;
-          if constexpr (kF32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
-          else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + to) = make_uint2(bf16_pair(o.x * f, o.y * f), bf16_pair(o.z * f, o.w * f));
-          if (a.lse && col == 0) a.lse[(int64_t)done.s * a.Hq + h0 + row] = (top + log2f(sum)) * 0.6931471805599453f;
-        } else {
-          *reinterpret_cast<float4*>(slot + row * D + col) = o;
-          if (col == 0) { slot[HT * D + row] = top; slot[HT * D + HT + row] = sum; }
-        }
-      }
-      __syncthreads();
-    };
-#pragma unroll
-    for (int half = 0; half < NT; ++half) {
-      if (8 * half >= rows) break;
-      if constexpr (kF32) {
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          float(&o)[4] = acc[8 * half + r];
+      if (ends || !more_chunks) {  // the sequence's last chunk, or the warp's
+        if constexpr (kF32) {
           if (D == 64) {  // the two halves of the warp had different keys
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] += __shfl_xor_sync(full, o[i], 16);
+            for (int r = 0; r < HT; ++r)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[r][i] += __shfl_xor_sync(full, acc[r][i], 16);
           }
-          if (8 * half + r < rows && (D == 128 || lane < 16)) *reinterpret_cast<float4*>(&part_o[warp][r][4 * lane]) = make_float4(o[0], o[1], o[2], o[3]);
-        }
-        if (lane >= 8 * half && lane < 8 * half + 8) { part_m[warp][lane - 8 * half] = m[0]; part_l[warp][lane - 8 * half] = l[0]; }
-      } else {
+        } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          float sum = l[2 * half + i];
-          sum += __shfl_xor_sync(full, sum, 4);
-          sum += __shfl_xor_sync(full, sum, 8);
-          sum += __shfl_xor_sync(full, sum, 16);
-          if (g == 0) { part_m[warp][2 * t + i] = m[2 * half + i]; part_l[warp][2 * t + i] = sum; }
-          if (8 * half + 2 * t + i < rows) {
-            constexpr bool kSplitRuns = kType == kTypeBf16 && D == 128;  // where the tiles' second dimensions lie
-#pragma unroll
-            for (int run = 0; run < 2; ++run)
-#pragma unroll
-              for (int j = 0; j < kTiles; j += 4) {
-                float v[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = acc[half * kTiles + j + k][2 * run + i];
-                const int col = (kSplitRuns ? 64 * run + 8 * g : (2 * g + run) * kTiles) + j;
-                *reinterpret_cast<float4*>(&part_o[warp][2 * t + i][col]) = make_float4(v[0], v[1], v[2], v[3]);
-              }
+          for (int h = 0; h < 2 * NT; ++h) {
+            l[h] += __shfl_xor_sync(full, l[h], 4);
+            l[h] += __shfl_xor_sync(full, l[h], 8);
+            l[h] += __shfl_xor_sync(full, l[h], 16);
           }
         }
+        const int first = x - cur.c;
+        if (first < w0) put_aside(cur, first, 2 * warp);
+        else if (ends) write_out(cur);
+        else put_aside(cur, first, 2 * warp + 1);
+        clear();
+        if (more_chunks) take_q(next);
       }
-      meet(half, whole);
+      cur = next;
     }
-    if (!whole) {
-      // The part is in the workspace.  The last of the sequence's blocks to arrive puts all parts together.  (The barrier at the end of meet() puts
-      // the block's writes before the arrival, whose release and acquire take them to the block that arrives last.)
-      const int b_first = block_of(done_first), n_parts = block_of(done_first + done.n - 1) - b_first + 1;
-      if (tid == 0) {
-        unsigned before;
-        asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.tickets + b_first) : "memory");
-        last_arrival = before + 1 == (unsigned)n_parts;
-        if (last_arrival) a.tickets[b_first] = 0;
+  }
+
+  // ---- the block's parts: put together where they are of one sequence, then written out, or, where other blocks have the rest, to the workspace
+  // Row `row` of the parts in `of`, by one warp: offset, sum and 4 dimensions per lane.
+  auto together = [&](unsigned of, int row, float& top, float& sum, float4& o) {
+    const float mine = (of >> lane) & 1 ? part_m[lane][row] : -CUDART_INF_F;
+    top = mine;
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(full, top, off));
+    const float weight = (of >> lane) & 1 ? exp2f(mine - top) : 0.f;
+    sum = (of >> lane) & 1 ? part_l[lane][row] * weight : 0.f;
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(full, sum, off);
+    o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (; of; of &= of - 1) {
+      const int i = __ffs(of) - 1;
+      const float f = __shfl_sync(full, weight, i);
+      const float4 v = *reinterpret_cast<const float4*>(part_of(i) + row * D + 4 * (D == 128 ? lane : lane & 15));
+      o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
+    }
+  };
+  auto write_row = [&](int s, int hi, int row, float top, float sum, const float4& o) {
+    const float f = (kF16 && a.cache.v_scale ? a.cache.v_scale[hi / a.tiles] : 1.f) / sum;
+    const int head = first_head(hi) + row;
+    const int64_t to = s * a.o_b + (int64_t)head * a.o_h + 4 * lane;
+    if (D == 128 || lane < 16) {
+      if constexpr (kF32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+      else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + to) = make_uint2(bf16_pair(o.x * f, o.y * f), bf16_pair(o.z * f, o.w * f));
+    }
+    if (a.lse && lane == 0) a.lse[(int64_t)s * a.Hq + head] = (top + log2f(sum)) * kLn2;
+  };
+  __syncthreads();
+  int shared_first[2], shared_last[2];  // parts at which a sequence of several blocks begins and ends in this one: at most two
+  int n_shared = 0;
+  {
+    const bool there = lane < 2 * NW && part_n[lane] > 0;
+    const unsigned valid = __ballot_sync(full, there);
+    const int id = there ? part_first[lane] : -1;  // sequences are told apart by their first chunk
+    const unsigned below = valid & ((1u << lane) - 1u);
+    const int id_before = __shfl_sync(full, id, below ? 31 - __clz(below) : lane);
+    const unsigned starts = __ballot_sync(full, there && (!below || id_before != id));
+    int turn = 0;  // rows are dealt to the warps in turn
+    for (unsigned st = starts; st; st &= st - 1) {
+      const int i = __ffs(st) - 1;
+      const unsigned rest = st & (st - 1), of = valid & ~((1u << i) - 1u) & (rest ? (rest & -rest) - 1u : 0xffffffffu);
+      const int s = part_s[i], hi = part_hi[i], first = part_first[i], rows = heads_of(hi);
+      const bool whole = first >= x0 && first + part_n[i] <= x1;
+      float* slot = a.parts + (2 * (int)blockIdx.x + (first < x0 ? 1 : 0)) * P::kSlot;
+      for (int row = (warp - turn + NW) % NW; row < rows; row += NW) {
+        float top, sum;
+        float4 o;
+        together(of, row, top, sum, o);
+        if (whole) {
+          write_row(s, hi, row, top, sum, o);
+        } else {
+          if (D == 128 || lane < 16) *reinterpret_cast<float4*>(slot + row * D + 4 * lane) = o;
+          if (lane == 0) { slot[HT * D + row] = top; slot[HT * D + HT + row] = sum; }
+        }
       }
-      __syncthreads();
-      if (last_arrival) {
-        auto part_at = [&](int i) { return a.parts + (2 * (b_first + i) + (i ? 1 : 0)) * P::kSlot; };
+      turn = (turn + rows) % NW;
+      if (!whole) {
+        shared_first[n_shared & 1] = i;
+        shared_last[n_shared & 1] = 31 - __clz(of);
+        ++n_shared;
+      }
+    }
+  }
+  // A sequence of several blocks: the last of them to arrive puts its parts together.  (The barrier puts the block's writes before
+  // the arrival, whose release and acquire take them to the block that arrives last.)
+  for (int k = 0; k < n_shared; ++k) {
+    const int i0 = shared_first[k & 1];
+    const int s = part_s[i0], hi = part_hi[i0], first = part_first[i0], rows = heads_of(hi);
+    const int b_first = block_of(first), n_parts = block_of(first + part_n[i0] - 1) - b_first + 1;
+    __syncthreads();
+    if (tid == 0) {
+      unsigned before;
+      asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.tickets + b_first) : "memory");
+      last_arrival = before + 1 == (unsigned)n_parts;
+      if (last_arrival) a.tickets[b_first] = 0;
+    }
+    __syncthreads();
+    if (!last_arrival) continue;
+    auto part_at = [&](int i) { return a.parts + (2 * (b_first + i) + (i ? 1 : 0)) * P::kSlot; };
+    // every warp puts parts warp, warp + NW, ... together, and then the warps theirs: in the shared memory of the warps' second parts
 #pragma unroll 1
-        for (int half = 0; half < NT; ++half) {
-          if (8 * half >= rows) break;
-          // this warp's parts: warp, warp + NW, ...; lane = (part in a group of 4, row)
-          constexpr int kRounds = (kTokenBlocks + 4 * NW - 1) / (4 * NW);
-          float pm[kRounds], top = -CUDART_INF_F, sum = 0.f;
-          const int r = lane & 7;
-          const bool row_ok = 8 * half + r < rows;
+    for (int half = 0; half < NT; ++half) {
+      if (8 * half >= rows) break;
+      constexpr int kRounds = (kTokenBlocks + 4 * NW - 1) / (4 * NW);
+      float pm[kRounds], top = -CUDART_INF_F, sum = 0.f;
+      const int r = 8 * half + (lane & 7);  // lane = (part in a group of 4, row)
 #pragma unroll
-          for (int k = 0; k < kRounds; ++k) {
-            const int i = warp + NW * (4 * k + (lane >> 3));
-            pm[k] = i < n_parts && row_ok ? __ldcg(part_at(i) + HT * D + 8 * half + r) : -CUDART_INF_F;
-            top = fmaxf(top, pm[k]);
+      for (int n = 0; n < kRounds; ++n) {
+        const int i = warp + NW * (4 * n + (lane >> 3));
+        pm[n] = i < n_parts && r < rows ? __ldcg(part_at(i) + HT * D + r) : -CUDART_INF_F;
+        top = fmaxf(top, pm[n]);
+      }
+      top = fmaxf(top, __shfl_xor_sync(full, top, 8));
+      top = fmaxf(top, __shfl_xor_sync(full, top, 16));
+#pragma unroll
+      for (int n = 0; n < kRounds; ++n) {
+        const int i = warp + NW * (4 * n + (lane >> 3));
+        const bool there = i < n_parts && r < rows;
+        pm[n] = there ? exp2f(pm[n] - top) : 0.f;
+        if (there) sum = fmaf(__ldcg(part_at(i) + HT * D + HT + r), pm[n], sum);
+      }
+      sum += __shfl_xor_sync(full, sum, 8);
+      sum += __shfl_xor_sync(full, sum, 16);
+      if (lane < 8) { part_m[2 * warp + 1][r] = top; part_l[2 * warp + 1][r] = sum; }
+      constexpr int kVec = 8 * D / 128;  // float4 of the 8 rows, per lane
+#pragma unroll
+      for (int v = 0; v < kVec; ++v) {
+        const int e = lane + 32 * v, row = e / (D / 4), col = 4 * (e % (D / 4));
+        if (8 * half + (32 * v) / (D / 4) >= rows) break;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int n = 0; n < kRounds; ++n)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int i = warp + NW * (4 * n + q);
+            const float f = __shfl_sync(full, pm[n], q * 8 + row);
+            if (i < n_parts && 8 * half + row < rows) {
+              const float4 x4 = __ldcg(reinterpret_cast<const float4*>(part_at(i) + (8 * half + row) * D + col));
+              o.x = fmaf(x4.x, f, o.x); o.y = fmaf(x4.y, f, o.y); o.z = fmaf(x4.z, f, o.z); o.w = fmaf(x4.w, f, o.w);
+            }
           }
-          top = fmaxf(top, __shfl_xor_sync(full, top, 8));
-          top = fmaxf(top, __shfl_xor_sync(full, top, 16));
-#pragma unroll
-          for (int k = 0; k < kRounds; ++k) {
-            const int i = warp + NW * (4 * k + (lane >> 3));
-            const bool there = i < n_parts && row_ok;
-            pm[k] = there ? exp2f(pm[k] - top) : 0.f;
-            if (there) sum = fmaf(__ldcg(part_at(i) + HT * D + HT + 8 * half + r), pm[k], sum);
-          }
-          sum += __shfl_xor_sync(full, sum, 8);
-          sum += __shfl_xor_sync(full, sum, 16);
-          if (lane < 8) { part_m[warp][lane] = top; part_l[warp][lane] = sum; }
-          constexpr int kVec = 8 * D / 128;  // float4 of the 8 rows, per lane
-#pragma unroll
-          for (int v = 0; v < kVec; ++v) {
-            const int e = lane + 32 * v, row = e / (D / 4), col = 4 * (e % (D / 4));
-            if (8 * half + (32 * v) / (D / 4) >= rows) break;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int k = 0; k < kRounds; ++k)
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                const int i = warp + NW * (4 * k + q);
-                const float f = __shfl_sync(full, pm[k], q * 8 + row);
-                if (i < n_parts && 8 * half + row < rows) {
-                  const float4 x4 = __ldcg(reinterpret_cast<const float4*>(part_at(i) + (8 * half + row) * D + col));
-                  o.x = fmaf(x4.x, f, o.x); o.y = fmaf(x4.y, f, o.y); o.z = fmaf(x4.z, f, o.z); o.w = fmaf(x4.w, f, o.w);
-                }
-              }
-            *reinterpret_cast<float4*>(&part_o[warp][row][col]) = o;
-          }
-          meet(half, true);
-        }
+        *reinterpret_cast<float4*>(part_of(2 * warp + 1) + (8 * half + row) * D + col) = o;
       }
     }
-    if constexpr (kF32) {
-      if (seg_end < x1) {
-        load_q(seg);
-        __syncthreads();
-      }
+    __syncthreads();
+    const unsigned of = 0xaaaaaaaau & (unsigned)((1ull << (2 * min(NW, n_parts))) - 1);
+    for (int row = warp; row < rows; row += NW) {
+      float top, sum;
+      float4 o;
+      together(of, row, top, sum, o);
+      write_row(s, hi, row, top, sum, o);
     }
-    pos = seg_end;
   }
   if (__any_sync(full, bad_page) && lane == 0 && a.status) atomicOr(a.status, TSD_STATUS_BAD_INDEX);
 }
