@@ -124,9 +124,10 @@ __device__ __forceinline__ uint32_t widen_hi(uint32_t w) {
 }
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-// Where a chunk lies: sequence, head tile of the sequence, chunk; chunks and keys of the sequence.
-struct Cursor {
-  int s, hi, c, n, len;
+// What a stretch of chunks is of: a sequence and a tile of the heads that share one of its kv heads.
+struct Item {
+  int s, kv, h0, rows;  // first of the query heads, how many
+  int len, n;           // keys, chunks
 };
 
 template <int D, int kType, int HT>
@@ -138,11 +139,12 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   constexpr bool kSplitRuns = kType == kTypeBf16 && D == 128;  // where the tiles' second dimensions lie
   constexpr int kAcc = kF32 ? HT : kTiles * NT;        // rows of 4 dimensions (fp32), or tiles of 16 dimensions x 8 heads
   extern __shared__ __align__(16) uint8_t dynamic[];
-  // Parts of the block's warps, two of each: of a sequence that begins before the warp's stretch (in shared memory of its own), and of one that
-  // goes on behind it (in the warp's queue, which is empty by then).  A sequence here is one of a head tile.
+  // Parts of the block's warps, two of each: of an item that begins before the warp's stretch (in shared memory of its own), and of one that
+  // goes on behind it (in the warp's queue, which is empty by then).
   auto part_of = [&](int i) { return reinterpret_cast<float*>(i & 1 ? dynamic + (i >> 1) * 8192 : dynamic + P::kQueue + (i >> 1) * P::kPart * 4); };
   __shared__ float part_m[2 * NW][HT], part_l[2 * NW][HT];
-  __shared__ int part_s[2 * NW], part_hi[2 * NW], part_first[2 * NW], part_n[2 * NW];  // whose: first chunk, chunks (0: no part)
+  __shared__ Item part_item[2 * NW];                          // whose (n = 0: no part)
+  __shared__ int part_first[2 * NW];                          // its first chunk
   __shared__ __align__(16) float weights[kF32 ? NW : 1][kF32 ? KC : 1][HT];
   __shared__ int last_arrival;
   static_assert(2 * NW <= 32, "a lane per part");
@@ -150,20 +152,23 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   constexpr unsigned full = 0xffffffffu;
   TokenParams a = p;
   grid_wait(a.cache.k, a.cache.v, a.cache.table, a.q, a.lens, a.cache.k_scale, a.cache.v_scale);
-  const int HI = a.Hkv * a.tiles;
+  const int HI = a.Hkv * a.tiles;  // items of a sequence
   auto length = [&](int s) { return a.lens ? min(max(a.lens[s], 0), a.cache.cap) : a.cache.cap; };
   auto chunks = [&](int len) { return (int)(((unsigned)len + KC - 1) / KC); };
 
   // ---- this block's share [x0, x1) of all chunks (fewer than 2^30: checked on the host)
   int total = 0;
   const int len0 = lane < a.S ? length(lane) : 0;  // of the first 32 sequences
+#pragma unroll 1
   for (int s = lane; s < a.S; s += 32) {
     const int n = chunks(s < 32 ? len0 : length(s));
     total += n;
     if (n == 0 && s % (int)gridDim.x == (int)blockIdx.x && warp == 0) {  // a sequence without keys
+#pragma unroll 1
       for (int h = 0; h < a.Hq; ++h) {
         if (a.lse) a.lse[(int64_t)s * a.Hq + h] = -CUDART_INF_F;
         uint4* o = reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.out) + (s * a.o_b + h * a.o_h) * (kF32 ? 4 : 2));
+#pragma unroll 1
         for (int i = 0; i < D * (kF32 ? 4 : 2) / 16; ++i) o[i] = make_uint4(0, 0, 0, 0);
       }
     }
@@ -174,19 +179,25 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   const int n_blocks = min((int)gridDim.x, (total + NW - 1) / NW);
   if ((int)blockIdx.x >= n_blocks) return;
   // blocks take total / n_blocks chunks each, the first `more` of them one more
-  const int each = total / n_blocks, more = total - each * n_blocks;
+  const int each = (int)((unsigned)total / (unsigned)n_blocks), more = total - each * n_blocks;
   auto first_of = [&](int b) { return b * each + min(b, more); };
-  auto block_of = [&](int x) { return x < more * (each + 1) ? x / (each + 1) : more + (x - more * (each + 1)) / each; };
+  auto block_of = [&](int x) {
+    const bool longer = x < more * (each + 1);
+    return (longer ? 0 : more) + (int)((unsigned)(longer ? x : x - more * (each + 1)) / (unsigned)(each + (longer ? 1 : 0)));
+  };
   const int x0 = first_of(blockIdx.x), x1 = first_of(blockIdx.x + 1);
   // and its warps an even share of that, [w0, w1) for this one
-  const int w0 = x0 + warp * ((x1 - x0) / NW) + min(warp, (x1 - x0) % NW), w1 = w0 + (x1 - x0) / NW + (warp < (x1 - x0) % NW ? 1 : 0);
+  const unsigned share = (unsigned)(x1 - x0) / NW, longer = (unsigned)(x1 - x0) % NW;
+  const int w0 = x0 + (int)(warp * share + min((unsigned)warp, longer)), w1 = w0 + (int)(share + (warp < (int)longer ? 1 : 0));
 
   // ---- where chunk w0 lies
-  Cursor cur;
+  Item next;       // the item whose chunk is fetched next, unless the one at hand goes on,
+  int next_c = 0;  // and that chunk
   {
     int before = 0;
-    cur.s = 0;
-    cur.len = 0;
+    next.s = 0;
+    next.len = 0;
+#pragma unroll 1
     for (int s0 = 0; s0 < a.S; s0 += 32) {
       const int len = s0 == 0 ? len0 : s0 + lane < a.S ? length(s0 + lane) : 0;
       const int mine = chunks(len) * HI;
@@ -199,56 +210,48 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
       const unsigned hit = __ballot_sync(full, before + upto > w0);
       if (hit) {
         const int l = __ffs(hit) - 1;
-        cur.s = s0 + l;
-        cur.len = __shfl_sync(full, len, l);
+        next.s = s0 + l;
+        next.len = __shfl_sync(full, len, l);
         before += __shfl_sync(full, upto - mine, l);
         break;
       }
       before += __shfl_sync(full, upto, 31);
     }
-    cur.n = max(chunks(cur.len), 1);
-    cur.hi = (w0 - before) / cur.n;
-    cur.c = (w0 - before) - cur.hi * cur.n;
+    next.n = max(chunks(next.len), 1);
+    const int hi = (int)((unsigned)(w0 - before) / (unsigned)next.n);
+    next_c = (w0 - before) - hi * next.n;
+    next.kv = a.tiles == 1 ? hi : (int)((unsigned)hi / (unsigned)a.tiles);
+    const int tile = hi - next.kv * a.tiles;
+    next.h0 = next.kv * a.group + tile * HT;
+    next.rows = min(HT, a.group - tile * HT);
   }
-  // to the next chunk
-  auto advance = [&](Cursor& c) {
-    if (++c.c < c.n) return;
-    c.c = 0;
-    if (++c.hi < HI) return;
-    c.hi = 0;
-    do {
-      if (++c.s >= a.S) {  // behind the last chunk: never fetched
-        c.n = 0x7fffffff;
-        c.len = 0;
-        return;
-      }
-      c.len = length(c.s);
-      c.n = chunks(c.len);
-    } while (c.n == 0);
+  auto item_after = [&](Item i) {
+    i.h0 += i.rows;
+    const int in_group = i.h0 - i.kv * a.group;  // heads of the kv head that are behind us
+    if (in_group == a.group && ++i.kv == a.Hkv) {
+      i.kv = i.h0 = 0;
+      do {
+        if (++i.s >= a.S) {  // behind the last chunk: never fetched
+          i.len = 0;
+          i.n = 0x7fffffff;
+          break;
+        }
+        i.len = length(i.s);
+        i.n = chunks(i.len);
+      } while (i.n == 0);
+    }
+    i.rows = min(HT, (i.kv + 1) * a.group - i.h0);
+    return i;
   };
 
   const int row_mask = (1 << a.cache.shift) - 1;
   const int64_t row_bytes = a.cache.ps_r * P::kSize, page_bytes = a.cache.ps_p * P::kSize, head_bytes = a.cache.ps_h * P::kSize;
   // lane i < NG: the table's entry for the chunk's keys [8 i, 8 i + 8)
-  auto entry_of = [&](const Cursor& c) {
-    const int key = c.c * KC + 8 * lane;
-    return lane < NG && key < c.len ? a.cache.table[c.s * a.cache.table_stride + (key >> a.cache.shift)] : -1;
-  };
-  // What fetching a chunk takes: lane i < NG, where its 8 keys begin (from k or v on), or -1 where there is no page; how many keys count.
-  struct Place {
-    int64_t at;
-    int left;
+  auto entry_of = [&](const Item& i, int c) {
+    const int key = c * KC + 8 * lane;
+    return lane < NG && key < i.len ? a.cache.table[i.s * a.cache.table_stride + (key >> a.cache.shift)] : -1;
   };
   bool bad_page = false;
-  auto place_of = [&](const Cursor& c, int entry) {
-    Place f;
-    f.left = c.len - c.c * KC;
-    const bool there = entry >= 0 && entry < a.cache.n_pages;
-    bad_page |= lane < NG && 8 * lane < f.left && !there;
-    const int key = c.c * KC + 8 * lane;
-    f.at = there ? (int64_t)entry * page_bytes + (int64_t)(key & row_mask) * row_bytes + (int64_t)(c.hi / a.tiles) * head_bytes : -1;
-    return f;
-  };
   // The warp's queue: 4 KB of K, 4 KB of V.  They are fetched along the rows (an instruction that touches whole 128-byte lines: in the order
   // in which the lanes want V, 32 bytes of a line at a time, the same loop without any arithmetic reads 5.0 TB/s instead of
   // 6.9) and read back in the products' order, 16-byte pieces of a 128-byte line exchanged by row so that both orders of reading are free
@@ -259,50 +262,45 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   const uint32_t queue_at = (uint32_t)__cvta_generic_to_shared(queue);
   const int my_row = lane / kLine, my_piece = lane % kLine;
   const int64_t lane_at = my_row * row_bytes + 16 * my_piece;
-  auto fetch = [&](const Place& f, const void* pages, uint32_t to) {
+  // `at`: lane i < NG, where the chunk's 8 keys from 8 i on begin (from k or v on), -1 where there is no page; `left`: how many keys count
+  auto fetch = [&](int64_t at, int left, const void* pages, uint32_t to) {
     const uint8_t* base = static_cast<const uint8_t*>(pages);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int row0 = i * kRowsAtOnce, row = row0 + my_row;
-      const int64_t at = __shfl_sync(full, f.at, row0 >> 3);
-      const bool wanted = at >= 0 && row < f.left;
-      fetch16(to + row * P::kRow + (my_piece ^ swizzle(row)) * 16, wanted ? base + at + lane_at + (row0 & 7) * row_bytes : base, wanted);
+      const int64_t from = __shfl_sync(full, at, row0 >> 3);
+      const bool wanted = from >= 0 && row < left;
+      fetch16(to + row * P::kRow + (my_piece ^ swizzle(row)) * 16, wanted ? base + from + lane_at + (row0 & 7) * row_bytes : base, wanted);
     }
   };
-  auto fetch_k = [&](const Place& f) { fetch(f, a.cache.k, queue_at); };
-  auto fetch_v = [&](const Place& f) { fetch(f, a.cache.v, queue_at + 4096); };
   // 16 bytes of a row of K (of V)
   auto k_piece = [&](int row, int i) { return *reinterpret_cast<const uint4*>(queue + row * P::kRow + (i ^ swizzle(row)) * 16); };
   auto v_piece = [&](int row, int i) { return *reinterpret_cast<const uint4*>(queue + 4096 + row * P::kRow + (i ^ swizzle(row)) * 16); };
 
-  // A head tile's heads: the first one, how many.
-  auto first_head = [&](int hi) { return hi / a.tiles * a.group + hi % a.tiles * HT; };
-  auto heads_of = [&](int hi) { return min(HT, a.group - hi % a.tiles * HT); };
   // the lane's part of the query rows of a (sequence, head tile): of head g (and g + 8), laid out as the keys are; fp32 reads them where they are
   uint32_t qr[kF32 ? 1 : NT][kF32 ? 1 : D / 8];
   float score_scale[kF16 ? 2 * NT : 1];  // e4m3: of the heads whose scores the lane gets
-  auto load_q = [&](const Cursor& c) {
+  auto load_q = [&](const Item& i) {
     if constexpr (!kF32) {
       constexpr int E = 16 / P::kSize;  // elements of a lane's piece
-      const int h0 = first_head(c.hi), rows = heads_of(c.hi);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int r = g + 8 * nt;
-        const __nv_bfloat16* row = static_cast<const __nv_bfloat16*>(a.q) + c.s * a.q_b + (int64_t)(h0 + r) * a.q_h;
+        const __nv_bfloat16* row = static_cast<const __nv_bfloat16*>(a.q) + i.s * a.q_b + (int64_t)(i.h0 + r) * a.q_h;
 #pragma unroll
         for (int pc = 0; pc < NP; ++pc)
 #pragma unroll
           for (int e = 0; e < E / 8; ++e) {
             uint4 v = make_uint4(0, 0, 0, 0);
-            if (r < rows) v = *reinterpret_cast<const uint4*>(row + pc * 4 * E + t * E + e * 8);
+            if (r < i.rows) v = *reinterpret_cast<const uint4*>(row + pc * 4 * E + t * E + e * 8);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) qr[nt][(pc * (E / 8) + e) * 4 + i] = word(v, i);
+            for (int k = 0; k < 4; ++k) qr[nt][(pc * (E / 8) + e) * 4 + k] = word(v, k);
           }
       }
     }
   };
-  auto take_q = [&](const Cursor& c) {
-    const float scale = a.scale_log2e * (kF16 && a.cache.k_scale ? a.cache.k_scale[c.hi / a.tiles] : 1.f);
+  auto take_q = [&](const Item& item) {
+    const float scale = a.scale_log2e * (kF16 && a.cache.k_scale ? a.cache.k_scale[item.kv] : 1.f);
     if constexpr (!kF16) {
       score_scale[0] = scale;
     } else {
@@ -336,11 +334,11 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(m) / 4); ++i) { m[i] = -CUDART_INF_F; l[i] = 0.f; }
   };
-  // What a sequence's chunks have come to so far: put aside as part i of the block, or, if they are all of it, written out.
-  auto put_aside = [&](const Cursor& c, int first, int i) {
+  // What an item's chunks have come to so far: put aside as part i of the block, or, if they are all of it, written out.
+  auto put_aside = [&](const Item& item, int first, int i) {
     float* o = part_of(i);
-    const int rows = heads_of(c.hi);
-    if (lane == 0) { part_s[i] = c.s; part_hi[i] = c.hi; part_first[i] = first; part_n[i] = c.n; }
+    const int rows = item.rows;
+    if (lane == 0) { part_item[i] = item; part_first[i] = first; }
     if constexpr (kF32) {
 #pragma unroll
       for (int r = 0; r < HT; ++r)
@@ -365,10 +363,10 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
       }
     }
   };
-  auto write_out = [&](const Cursor& c) {
-    const int h0 = first_head(c.hi), rows = heads_of(c.hi);
-    const float v_scale = kF16 && a.cache.v_scale ? a.cache.v_scale[c.hi / a.tiles] : 1.f;
-    const int64_t to = c.s * a.o_b + (int64_t)h0 * a.o_h, lse_to = (int64_t)c.s * a.Hq + h0;
+  auto write_out = [&](const Item& item) {
+    const int rows = item.rows;
+    const float v_scale = kF16 && a.cache.v_scale ? a.cache.v_scale[item.kv] : 1.f;
+    const int64_t to = item.s * a.o_b + (int64_t)item.h0 * a.o_h, lse_to = (int64_t)item.s * a.Hq + item.h0;
     if constexpr (kF32) {
 #pragma unroll
       for (int r = 0; r < HT; ++r) {
@@ -382,7 +380,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
       for (int h = 0; h < 2 * NT; ++h) {
         const int head = 8 * (h >> 1) + 2 * t + (h & 1);
         if (head < rows) {
-          const float f = v_scale / l[h];
+          const float f = __fdividef(v_scale, l[h]);  // 2 ulp
           __nv_bfloat16* row = static_cast<__nv_bfloat16*>(a.out) + to + head * a.o_h;
 #pragma unroll
           for (int run = 0; run < 2; ++run) {
@@ -394,89 +392,117 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
             if constexpr (kTiles == 8) *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
             else *reinterpret_cast<uint2*>(at) = make_uint2(w[0], w[1]);
           }
-          if (a.lse && g == 0) a.lse[lse_to + head] = (m[h] + log2f(l[h])) * kLn2;
+          if (a.lse && g == 0) a.lse[lse_to + head] = (m[h] + __log2f(l[h])) * kLn2;
         }
       }
     }
   };
 
-  // ---- the warp's first chunk
-  if (lane < 2) part_n[2 * warp + lane] = 0;
-  Place here{-1, 0};        // of the chunk in the queue
-  int entry = -1;           // the table's entries for the chunk that is fetched next
-  if (w0 < w1) {
-    here = place_of(cur, entry_of(cur));
-    fetch_k(here);
-    fetch_commit();
-    fetch_v(here);
-    fetch_commit();
-    load_q(cur);
-    Cursor next = cur;
-    advance(next);
-    if (w0 + 1 < w1) entry = entry_of(next);
-    take_q(cur);
-  }
-  clear();
-  {
-    for (int x = w0; x < w1; ++x) {
-      const int left = here.left;  // keys of the chunk that count: 1 and up
-      const int rows = heads_of(cur.hi);
-      // two groups of fetches are under way, this chunk's K and its V; further down its V and the next one's K
+  // ---- the warp's chunks.  The round before the first one only fetches.
+  if (lane < 2) part_item[2 * warp + lane].n = 0;
+  __syncwarp();
+  Item item = next;                                     // at hand, and its chunk;
+  int c = 0, left = 0;                                  // how many of the chunk's keys count
+  int entry = -1;                                       // the table's entries for the chunk behind it,
+  int next_entry = w0 < w1 ? entry_of(next, next_c) : -1;  // and for the next item's
+  bool fresh = false;                                   // the item's queries have just been asked for
+#pragma unroll 1
+  for (int x = w0 - 1; x < w1; ++x) {
+    const bool real = x >= w0, more_chunks = x + 1 < w1, ends = !real || c + 1 == item.n;  // of the warp; the item
+    const int rows = item.rows;
+    int64_t at = -1;
+    int then = 0, then_left = 0;  // the chunk that is fetched in this round
+    auto fetch_next_k = [&] {
+      if (more_chunks) {
+        then = ends ? next_c : c + 1;
+        const int kv = ends ? next.kv : item.kv, e = ends ? next_entry : entry, key = then * KC + 8 * lane;
+        then_left = (ends ? next.len : item.len) - then * KC;
+        const bool there = e >= 0 && e < a.cache.n_pages;
+        bad_page |= lane < NG && 8 * lane < then_left && !there;
+        at = there ? (int64_t)e * page_bytes + (int64_t)(key & row_mask) * row_bytes + (int64_t)kv * head_bytes : -1;
+        fetch(at, then_left, a.cache.k, queue_at);
+        if (ends) load_q(next);
+      }
+      fetch_commit();
+    };
+    auto fetch_next_v = [&] {
+      if (more_chunks) {
+        fetch(at, then_left, a.cache.v, queue_at + 4096);
+        if (ends) entry = entry_of(next, then + 1);
+        else entry = entry_of(item, then + 1);
+      }
+      fetch_commit();
+    };
+    // While a chunk is worked on, two groups of fetches are under way: its K and its V, then its V and the next one's K.
+    float sc[kF32 ? 1 : NG / 2][NT][4];  // scores of keys 16 mt + g and + 8, heads 8 nt + 2t and + 1; then the weights
+    if (real) {
       fetch_wait<1>();
       __syncwarp();
-      const bool more_chunks = x + 1 < w1, ends = cur.c + 1 == cur.n;  // of the warp; the sequence
-      Cursor next = cur;
-      auto k_used = [&] {  // the next chunk's K takes its place
-        __syncwarp();
-        advance(next);
-        if (more_chunks) {
-          here = place_of(next, entry);
-          fetch_k(here);
-          if (ends) load_q(next);
-        }
-        fetch_commit();
-        fetch_wait<1>();
-        __syncwarp();
-      };
-      auto v_used = [&] {
-        __syncwarp();
-        if (more_chunks) {
-          fetch_v(here);
-          Cursor then = next;
-          advance(then);
-          if (x + 2 < w1) entry = entry_of(then);
-        }
-        fetch_commit();
-      };
+      if (fresh) {
+        clear();
+        take_q(item);
+      }
       if constexpr (!kF32) {
-        // ---------------------------------------------------------------- scores of keys 16 mt + g and + 8, heads 8 nt + 2t and + 1
-        float sc[NG / 2][NT][4];
+        // ---------------------------------------------------------------- scores
 #pragma unroll
         for (int mt = 0; mt < NG / 2; ++mt)
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) sc[mt][nt][0] = sc[mt][nt][1] = sc[mt][nt][2] = sc[mt][nt][3] = 0.f;
 #pragma unroll
-        for (int c = 0; c < NP; ++c) {
+        for (int pc = 0; pc < NP; ++pc) {
 #pragma unroll
           for (int mt = 0; mt < NG / 2; ++mt) {
-            const uint4 k0 = k_piece(16 * mt + g, 4 * c + t), k8 = k_piece(16 * mt + 8 + g, 4 * c + t);
+            const uint4 k0 = k_piece(16 * mt + g, 4 * pc + t), k8 = k_piece(16 * mt + 8 + g, 4 * pc + t);
             if constexpr (kType == kTypeBf16) {
 #pragma unroll
               for (int e = 0; e < 2; ++e)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
-                  mma<kF16>(sc[mt][nt], word(k0, 2 * e), word(k8, 2 * e), word(k0, 2 * e + 1), word(k8, 2 * e + 1), qr[nt][c * 4 + 2 * e], qr[nt][c * 4 + 2 * e + 1]);
+                  mma<kF16>(sc[mt][nt], word(k0, 2 * e), word(k8, 2 * e), word(k0, 2 * e + 1), word(k8, 2 * e + 1), qr[nt][pc * 4 + 2 * e], qr[nt][pc * 4 + 2 * e + 1]);
             } else {
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 const uint32_t a0 = widen_lo(word(k0, e)), a1 = widen_lo(word(k8, e)), a2 = widen_hi(word(k0, e)), a3 = widen_hi(word(k8, e));
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<kF16>(sc[mt][nt], a0, a1, a2, a3, qr[nt][c * 8 + 2 * e], qr[nt][c * 8 + 2 * e + 1]);
+                for (int nt = 0; nt < NT; ++nt) mma<kF16>(sc[mt][nt], a0, a1, a2, a3, qr[nt][pc * 8 + 2 * e], qr[nt][pc * 8 + 2 * e + 1]);
               }
             }
           }
         }
-        k_used();
+      } else {
+        // ---------------------------------------------------------------- fp32 scores: 4 lanes per key
+        const float* q32 = static_cast<const float*>(a.q) + item.s * a.q_b + (int64_t)item.h0 * a.q_h;
+#pragma unroll
+        for (int nb = 0; nb < NG; ++nb) {
+          uint4 kr[NP];
+#pragma unroll
+          for (int pc = 0; pc < NP; ++pc) kr[pc] = k_piece(8 * nb + g, 4 * pc + t);
+#pragma unroll
+          for (int r = 0; r < HT; ++r) {
+            if (r < rows) {
+              float z = 0.f;
+#pragma unroll
+              for (int pc = 0; pc < NP; ++pc) {
+                const float4 qv = __ldg(reinterpret_cast<const float4*>(q32 + r * a.q_h + 16 * pc + 4 * t));
+                z = fmaf(qv.x, __uint_as_float(kr[pc].x), z);
+                z = fmaf(qv.y, __uint_as_float(kr[pc].y), z);
+                z = fmaf(qv.z, __uint_as_float(kr[pc].z), z);
+                z = fmaf(qv.w, __uint_as_float(kr[pc].w), z);
+              }
+              z += __shfl_xor_sync(full, z, 1);
+              z += __shfl_xor_sync(full, z, 2);
+              if (t == 0) weights[warp][8 * nb + g][r] = 8 * nb + g < left ? z * score_scale[0] : -CUDART_INF_F;
+            }
+          }
+        }
+      }
+      __syncwarp();
+    }
+    fetch_next_k();  // in the place of the K that has been used
+    if (real) {
+      fetch_wait<1>();
+      __syncwarp();
+      if constexpr (!kF32) {
         // ---------------------------------------------------------------- weights
         bool passed = false;
 #pragma unroll
@@ -588,35 +614,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
             }
           }
         }
-        v_used();
       } else {
-        // ---------------------------------------------------------------- fp32 scores: 4 lanes per key
-        const float* q32 = static_cast<const float*>(a.q) + cur.s * a.q_b + (int64_t)first_head(cur.hi) * a.q_h;
-#pragma unroll
-        for (int nb = 0; nb < NG; ++nb) {
-          uint4 kr[NP];
-#pragma unroll
-          for (int c = 0; c < NP; ++c) kr[c] = k_piece(8 * nb + g, 4 * c + t);
-#pragma unroll
-          for (int r = 0; r < HT; ++r) {
-            if (r < rows) {
-              float z = 0.f;
-#pragma unroll
-              for (int c = 0; c < NP; ++c) {
-                const float4 qv = __ldg(reinterpret_cast<const float4*>(q32 + r * a.q_h + 16 * c + 4 * t));
-                z = fmaf(qv.x, __uint_as_float(kr[c].x), z);
-                z = fmaf(qv.y, __uint_as_float(kr[c].y), z);
-                z = fmaf(qv.z, __uint_as_float(kr[c].z), z);
-                z = fmaf(qv.w, __uint_as_float(kr[c].w), z);
-              }
-              z += __shfl_xor_sync(full, z, 1);
-              z += __shfl_xor_sync(full, z, 2);
-              if (t == 0) weights[warp][8 * nb + g][r] = 8 * nb + g < left ? z * score_scale[0] : -CUDART_INF_F;
-            }
-          }
-        }
-        k_used();
-        __syncwarp();
         // row lane % HT, keys lane / HT, + 32 / HT, ...
         {
           constexpr int KL = 32 / HT;  // keys that the lanes take at once
@@ -672,10 +670,12 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
             }
           }
         }
-        v_used();
-        __syncwarp();
       }
-      if (ends || !more_chunks) {  // the sequence's last chunk, or the warp's
+      __syncwarp();
+    }
+    fetch_next_v();
+    if (real) {
+      if (ends || !more_chunks) {  // the item's last chunk, or the warp's
         if constexpr (kF32) {
           if (D == 64) {  // the two halves of the warp had different keys
 #pragma unroll
@@ -691,88 +691,111 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
             l[h] += __shfl_xor_sync(full, l[h], 16);
           }
         }
-        const int first = x - cur.c;
-        if (first < w0) put_aside(cur, first, 2 * warp);
-        else if (ends) write_out(cur);
-        else put_aside(cur, first, 2 * warp + 1);
-        clear();
-        if (more_chunks) take_q(next);
+        const int first = x - c;
+        if (first < w0) put_aside(item, first, 2 * warp);
+        else if (ends) write_out(item);
+        else put_aside(item, first, 2 * warp + 1);
       }
-      cur = next;
+    }
+    left = then_left;
+    c = then;
+    fresh = ends;
+    if (ends && more_chunks) {
+      item = next;
+      next = item_after(next);
+      next_c = 0;
+      next_entry = entry_of(next, 0);
     }
   }
 
   // ---- the block's parts: put together where they are of one sequence, then written out, or, where other blocks have the rest, to the workspace
   // Row `row` of the parts in `of`, by one warp: offset, sum and 4 dimensions per lane.
   auto together = [&](unsigned of, int row, float& top, float& sum, float4& o) {
-    const float mine = (of >> lane) & 1 ? part_m[lane][row] : -CUDART_INF_F;
+    const bool in = (of >> lane) & 1;
+    const float mine = in ? part_m[lane][row] : -CUDART_INF_F;
     top = mine;
 #pragma unroll
     for (int off = 16; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(full, top, off));
-    const float weight = (of >> lane) & 1 ? exp2f(mine - top) : 0.f;
-    sum = (of >> lane) & 1 ? part_l[lane][row] * weight : 0.f;
+    const float weight = in ? exp2_approx(mine - top) : 0.f;
+    sum = in ? part_l[lane][row] * weight : 0.f;
 #pragma unroll
     for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(full, sum, off);
     o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (; of; of &= of - 1) {
-      const int i = __ffs(of) - 1;
-      const float f = __shfl_sync(full, weight, i);
-      const float4 v = *reinterpret_cast<const float4*>(part_of(i) + row * D + 4 * (D == 128 ? lane : lane & 15));
-      o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
+#pragma unroll 1
+    while (of) {  // four at a time
+      float4 v[4];
+      float f[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = of ? __ffs(of) - 1 : 0;
+        f[k] = __shfl_sync(full, weight, i);
+        if (!of) f[k] = 0.f;
+        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (of) v[k] = *reinterpret_cast<const float4*>(part_of(i) + row * D + 4 * (D == 128 ? lane : lane & 15));
+        of &= of - 1;  // 0 stays 0
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        o.x = fmaf(v[k].x, f[k], o.x); o.y = fmaf(v[k].y, f[k], o.y); o.z = fmaf(v[k].z, f[k], o.z); o.w = fmaf(v[k].w, f[k], o.w);
+      }
     }
   };
-  auto write_row = [&](int s, int hi, int row, float top, float sum, const float4& o) {
-    const float f = (kF16 && a.cache.v_scale ? a.cache.v_scale[hi / a.tiles] : 1.f) / sum;
-    const int head = first_head(hi) + row;
-    const int64_t to = s * a.o_b + (int64_t)head * a.o_h + 4 * lane;
+  auto write_row = [&](const Item& item, int row, float top, float sum, const float4& o) {
+    const float v_scale = kF16 && a.cache.v_scale ? a.cache.v_scale[item.kv] : 1.f, f = kF32 ? v_scale / sum : __fdividef(v_scale, sum);
+    const int head = item.h0 + row;
+    const int64_t to = item.s * a.o_b + (int64_t)head * a.o_h + 4 * lane;
     if (D == 128 || lane < 16) {
       if constexpr (kF32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
       else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + to) = make_uint2(bf16_pair(o.x * f, o.y * f), bf16_pair(o.z * f, o.w * f));
     }
-    if (a.lse && lane == 0) a.lse[(int64_t)s * a.Hq + head] = (top + log2f(sum)) * kLn2;
+    if (a.lse && lane == 0) a.lse[(int64_t)item.s * a.Hq + head] = (top + log2f(sum)) * kLn2;
   };
   __syncthreads();
-  int shared_first[2], shared_last[2];  // parts at which a sequence of several blocks begins and ends in this one: at most two
-  int n_shared = 0;
+  int shared0 = 0, shared1 = 0, n_shared = 0;  // parts with which items of several blocks begin in this one: at most two
   {
-    const bool there = lane < 2 * NW && part_n[lane] > 0;
+    const bool there = lane < 2 * NW && part_item[lane].n > 0;
     const unsigned valid = __ballot_sync(full, there);
-    const int id = there ? part_first[lane] : -1;  // sequences are told apart by their first chunk
+    const int id = there ? part_first[lane] : -1;  // items are told apart by their first chunk
     const unsigned below = valid & ((1u << lane) - 1u);
     const int id_before = __shfl_sync(full, id, below ? 31 - __clz(below) : lane);
     const unsigned starts = __ballot_sync(full, there && (!below || id_before != id));
     int turn = 0;  // rows are dealt to the warps in turn
+#pragma unroll 1
     for (unsigned st = starts; st; st &= st - 1) {
       const int i = __ffs(st) - 1;
       const unsigned rest = st & (st - 1), of = valid & ~((1u << i) - 1u) & (rest ? (rest & -rest) - 1u : 0xffffffffu);
-      const int s = part_s[i], hi = part_hi[i], first = part_first[i], rows = heads_of(hi);
-      const bool whole = first >= x0 && first + part_n[i] <= x1;
+      const Item it = part_item[i];
+      const int first = part_first[i], rows = it.rows;
+      const bool whole = first >= x0 && first + it.n <= x1;
       float* slot = a.parts + (2 * (int)blockIdx.x + (first < x0 ? 1 : 0)) * P::kSlot;
-      for (int row = (warp - turn + NW) % NW; row < rows; row += NW) {
+#pragma unroll 1
+      for (int row = warp >= turn ? warp - turn : warp - turn + NW; row < rows; row += NW) {
         float top, sum;
         float4 o;
         together(of, row, top, sum, o);
         if (whole) {
-          write_row(s, hi, row, top, sum, o);
+          write_row(it, row, top, sum, o);
         } else {
           if (D == 128 || lane < 16) *reinterpret_cast<float4*>(slot + row * D + 4 * lane) = o;
           if (lane == 0) { slot[HT * D + row] = top; slot[HT * D + HT + row] = sum; }
         }
       }
-      turn = (turn + rows) % NW;
+      turn += rows;
+      if (turn >= NW) turn -= NW;
       if (!whole) {
-        shared_first[n_shared & 1] = i;
-        shared_last[n_shared & 1] = 31 - __clz(of);
+        if (n_shared == 0) shared0 = i;
+        else shared1 = i;
         ++n_shared;
       }
     }
   }
-  // A sequence of several blocks: the last of them to arrive puts its parts together.  (The barrier puts the block's writes before
+  // An item of several blocks: the last of them to arrive puts its parts together.  (The barrier puts the block's writes before
   // the arrival, whose release and acquire take them to the block that arrives last.)
+#pragma unroll 1
   for (int k = 0; k < n_shared; ++k) {
-    const int i0 = shared_first[k & 1];
-    const int s = part_s[i0], hi = part_hi[i0], first = part_first[i0], rows = heads_of(hi);
-    const int b_first = block_of(first), n_parts = block_of(first + part_n[i0] - 1) - b_first + 1;
+    const int i0 = k == 0 ? shared0 : shared1;
+    const Item it = part_item[i0];
+    const int first = part_first[i0], rows = it.rows, b_first = block_of(first), n_parts = block_of(first + it.n - 1) - b_first + 1;
     __syncthreads();
     if (tid == 0) {
       unsigned before;
@@ -782,59 +805,56 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
     }
     __syncthreads();
     if (!last_arrival) continue;
-    auto part_at = [&](int i) { return a.parts + (2 * (b_first + i) + (i ? 1 : 0)) * P::kSlot; };
-    // every warp puts parts warp, warp + NW, ... together, and then the warps theirs: in the shared memory of the warps' second parts
+    // A row by `subs` warps, each with parts sub, sub + subs, ...: 32 of them at a time, a lane for the offset and sum of each.  What the
+    // warps come to meets in the shared memory of their second parts.
+    const int subs = max(1, NW / rows);
 #pragma unroll 1
-    for (int half = 0; half < NT; ++half) {
-      if (8 * half >= rows) break;
-      constexpr int kRounds = (kTokenBlocks + 4 * NW - 1) / (4 * NW);
-      float pm[kRounds], top = -CUDART_INF_F, sum = 0.f;
-      const int r = 8 * half + (lane & 7);  // lane = (part in a group of 4, row)
+    for (int task = warp; task < rows * subs; task += NW) {
+      const int row = task % rows, sub = task / rows;
+      float top = -CUDART_INF_F, sum = 0.f;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      auto part_at = [&](int i) { return a.parts + (2 * (b_first + i) + (i ? 1 : 0)) * P::kSlot; };
+#pragma unroll 1
+      for (int i0 = sub; i0 < n_parts; i0 += 32 * subs) {
+        const int i = i0 + lane * subs, count = min(32, (n_parts - i0 + subs - 1) / subs);
+        const float mine = lane < count ? __ldcg(part_at(i) + HT * D + row) : -CUDART_INF_F;
+        const float sum_mine = lane < count ? __ldcg(part_at(i) + HT * D + HT + row) : 0.f;
+        float to = mine;
 #pragma unroll
-      for (int n = 0; n < kRounds; ++n) {
-        const int i = warp + NW * (4 * n + (lane >> 3));
-        pm[n] = i < n_parts && r < rows ? __ldcg(part_at(i) + HT * D + r) : -CUDART_INF_F;
-        top = fmaxf(top, pm[n]);
-      }
-      top = fmaxf(top, __shfl_xor_sync(full, top, 8));
-      top = fmaxf(top, __shfl_xor_sync(full, top, 16));
+        for (int off = 16; off >= 1; off >>= 1) to = fmaxf(to, __shfl_xor_sync(full, to, off));
+        to = fmaxf(to, top);
+        const float alpha = top == to ? 1.f : exp2_approx(top - to), weight = lane < count ? exp2_approx(mine - to) : 0.f;
+        top = to;
+        float all = sum_mine * weight;
 #pragma unroll
-      for (int n = 0; n < kRounds; ++n) {
-        const int i = warp + NW * (4 * n + (lane >> 3));
-        const bool there = i < n_parts && r < rows;
-        pm[n] = there ? exp2f(pm[n] - top) : 0.f;
-        if (there) sum = fmaf(__ldcg(part_at(i) + HT * D + HT + r), pm[n], sum);
-      }
-      sum += __shfl_xor_sync(full, sum, 8);
-      sum += __shfl_xor_sync(full, sum, 16);
-      if (lane < 8) { part_m[2 * warp + 1][r] = top; part_l[2 * warp + 1][r] = sum; }
-      constexpr int kVec = 8 * D / 128;  // float4 of the 8 rows, per lane
+        for (int off = 16; off >= 1; off >>= 1) all += __shfl_xor_sync(full, all, off);
+        sum = fmaf(sum, alpha, all);
+        o.x *= alpha; o.y *= alpha; o.z *= alpha; o.w *= alpha;
+#pragma unroll 1
+        for (int j = 0; j < count; j += 8) {
+          float4 v[8];
 #pragma unroll
-      for (int v = 0; v < kVec; ++v) {
-        const int e = lane + 32 * v, row = e / (D / 4), col = 4 * (e % (D / 4));
-        if (8 * half + (32 * v) / (D / 4) >= rows) break;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int u = 0; u < 8; ++u)
+            v[u] = j + u < count ? __ldcg(reinterpret_cast<const float4*>(part_at(i0 + (j + u) * subs) + row * D + 4 * (D == 128 ? lane : lane & 15)))
+                                 : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int n = 0; n < kRounds; ++n)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int i = warp + NW * (4 * n + q);
-            const float f = __shfl_sync(full, pm[n], q * 8 + row);
-            if (i < n_parts && 8 * half + row < rows) {
-              const float4 x4 = __ldcg(reinterpret_cast<const float4*>(part_at(i) + (8 * half + row) * D + col));
-              o.x = fmaf(x4.x, f, o.x); o.y = fmaf(x4.y, f, o.y); o.z = fmaf(x4.z, f, o.z); o.w = fmaf(x4.w, f, o.w);
-            }
+          for (int u = 0; u < 8; ++u) {
+            const float f = __shfl_sync(full, weight, (j + u) & 31);  // 0 behind the last
+            o.x = fmaf(v[u].x, f, o.x); o.y = fmaf(v[u].y, f, o.y); o.z = fmaf(v[u].z, f, o.z); o.w = fmaf(v[u].w, f, o.w);
           }
-        *reinterpret_cast<float4*>(part_of(2 * warp + 1) + (8 * half + row) * D + col) = o;
+        }
       }
+      if (D == 128 || lane < 16) *reinterpret_cast<float4*>(part_of(2 * sub + 1) + row * D + 4 * lane) = o;
+      if (lane == 0) { part_m[2 * sub + 1][row] = top; part_l[2 * sub + 1][row] = sum; }
     }
     __syncthreads();
-    const unsigned of = 0xaaaaaaaau & (unsigned)((1ull << (2 * min(NW, n_parts))) - 1);
+    const unsigned of = 0xaaaaaaaau & (unsigned)((1ull << (2 * min(subs, n_parts))) - 1);
+#pragma unroll 1
     for (int row = warp; row < rows; row += NW) {
       float top, sum;
       float4 o;
       together(of, row, top, sum, o);
-      write_row(s, hi, row, top, sum, o);
+      write_row(it, row, top, sum, o);
     }
   }
   if (__any_sync(full, bad_page) && lane == 0 && a.status) atomicOr(a.status, TSD_STATUS_BAD_INDEX);
