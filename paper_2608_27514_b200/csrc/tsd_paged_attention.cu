@@ -57,7 +57,7 @@ struct TokenParams {
   int64_t q_b, q_h, o_b, o_h;
   int S, Hq, Hkv, group, tiles;  // tiles: of HT heads per kv head
   float scale_log2e;
-  float* parts;        // [2 * blocks] slots: a block's last stretch (even), its first where that began in a block before (odd)
+  float* parts;        // [2 * blocks] slots: a block's part of the item that began in a block before it (even), of one that goes on behind it (odd)
   unsigned* tickets;   // per block in which a shared sequence begins
   uint32_t* status;
 };
@@ -161,31 +161,21 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   const int len0 = lane < a.S ? length(lane) : 0;  // of the first 32 sequences
 #pragma unroll 1
   for (int s = lane; s < a.S; s += 32) {
-    const int n = chunks(s < 32 ? len0 : length(s));
-    total += n;
-    if (n == 0 && s % (int)gridDim.x == (int)blockIdx.x && warp == 0) {  // a sequence without keys
-#pragma unroll 1
-      for (int h = 0; h < a.Hq; ++h) {
-        if (a.lse) a.lse[(int64_t)s * a.Hq + h] = -CUDART_INF_F;
-        uint4* o = reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.out) + (s * a.o_b + h * a.o_h) * (kF32 ? 4 : 2));
-#pragma unroll 1
-        for (int i = 0; i < D * (kF32 ? 4 : 2) / 16; ++i) o[i] = make_uint4(0, 0, 0, 0);
-      }
-    }
+    total += chunks(s < 32 ? len0 : length(s));
   }
 #pragma unroll
   for (int off = 16; off >= 1; off >>= 1) total += __shfl_xor_sync(full, total, off);
   total *= HI;
-  const int n_blocks = min((int)gridDim.x, (total + NW - 1) / NW);
-  if ((int)blockIdx.x >= n_blocks) return;
-  // blocks take total / n_blocks chunks each, the first `more` of them one more
+  // blocks (as many as have a chunk for each of their warps) take total / n_blocks chunks each, the first `more` of them one more
+  const int n_blocks = max(1, min((int)gridDim.x, (total + NW - 1) / NW));
   const int each = (int)((unsigned)total / (unsigned)n_blocks), more = total - each * n_blocks;
   auto first_of = [&](int b) { return b * each + min(b, more); };
   auto block_of = [&](int x) {
     const bool longer = x < more * (each + 1);
     return (longer ? 0 : more) + (int)((unsigned)(longer ? x : x - more * (each + 1)) / (unsigned)(each + (longer ? 1 : 0)));
   };
-  const int x0 = first_of(blockIdx.x), x1 = first_of(blockIdx.x + 1);
+  const bool idle = (int)blockIdx.x >= n_blocks;
+  const int x0 = idle ? total : first_of(blockIdx.x), x1 = idle ? total : first_of(blockIdx.x + 1);
   // and its warps an even share of that, [w0, w1) for this one
   const unsigned share = (unsigned)(x1 - x0) / NW, longer = (unsigned)(x1 - x0) % NW;
   const int w0 = x0 + (int)(warp * share + min((unsigned)warp, longer)), w1 = w0 + (int)(share + (warp < (int)longer ? 1 : 0));
@@ -257,25 +247,39 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   // 6.9) and read back in the products' order, 16-byte pieces of a 128-byte line exchanged by row so that both orders of reading are free
   // of bank conflicts (8 lanes read 4 pieces of 2 rows of K, 2 pieces of 4 rows of V).
   constexpr int kLine = P::kRow / 16, kRowsAtOnce = 32 / kLine;  // pieces per row, rows per instruction
-  auto swizzle = [](int row) { return P::kRow == 64 ? (row >> 1) & 3 : ((row ^ (row >> 1)) & 1) << 2 | ((row >> 2) & 1) << 1; };
+  constexpr auto swizzle = [](int row) {                         // what a row's pieces are exchanged by: linear in the row's bits
+    return P::kRow == 64 ? (row >> 1) & 3 : ((row ^ (row >> 1)) & 1) << 2 | ((row >> 2) & 1) << 1;
+  };
   uint8_t* const queue = dynamic + warp * 8192;
-  const uint32_t queue_at = (uint32_t)__cvta_generic_to_shared(queue);
   const int my_row = lane / kLine, my_piece = lane % kLine;
-  const int64_t lane_at = my_row * row_bytes + 16 * my_piece;
+  const uint32_t lane_to = my_row * P::kRow + (my_piece ^ swizzle(my_row)) * 16;
+  const uint32_t queue_at = (uint32_t)__cvta_generic_to_shared(queue);
+  const int64_t lane_from = my_row * row_bytes + 16 * my_piece;
   // `at`: lane i < NG, where the chunk's 8 keys from 8 i on begin (from k or v on), -1 where there is no page; `left`: how many keys count
   auto fetch = [&](int64_t at, int left, const void* pages, uint32_t to) {
-    const uint8_t* base = static_cast<const uint8_t*>(pages);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int row0 = i * kRowsAtOnce, row = row0 + my_row;
-      const int64_t from = __shfl_sync(full, at, row0 >> 3);
-      const bool wanted = from >= 0 && row < left;
-      fetch16(to + row * P::kRow + (my_piece ^ swizzle(row)) * 16, wanted ? base + from + lane_at + (row0 & 7) * row_bytes : base, wanted);
+    for (int nb = 0; nb < NG; ++nb) {
+      const int64_t from = __shfl_sync(full, at, nb);
+      const uint8_t* p = static_cast<const uint8_t*>(pages) + (from < 0 ? 0 : from) + lane_from;
+      const int here = from < 0 ? 0 : left - 8 * nb - my_row;  // how many of the group's keys, from this lane's first one on
+#pragma unroll
+      for (int j = 0; j < 8 / kRowsAtOnce; ++j) {
+        const int row0 = 8 * nb + j * kRowsAtOnce;
+        fetch16(to + (lane_to ^ (swizzle(row0) * 16)) + row0 * P::kRow, p, j * kRowsAtOnce < here);
+        p += kRowsAtOnce * row_bytes;
+      }
     }
   };
-  // 16 bytes of a row of K (of V)
-  auto k_piece = [&](int row, int i) { return *reinterpret_cast<const uint4*>(queue + row * P::kRow + (i ^ swizzle(row)) * 16); };
-  auto v_piece = [&](int row, int i) { return *reinterpret_cast<const uint4*>(queue + 4096 + row * P::kRow + (i ^ swizzle(row)) * 16); };
+  // K: 16 bytes at 64 pc + 16 t of key 8 nb + g.  V: of the lane's keys 16 mt + 2t + {0, 1, 8, 9}, number i, 16 bytes at 128 h + 16 g (rows of 64
+  // bytes: the 16 that hold its 8)
+  const uint8_t* const k_lane = queue + g * P::kRow;
+  const int k_to = (t ^ swizzle(g)) * 16;
+  const uint8_t* const v_lane = queue + 4096 + 2 * t * P::kRow;
+  const int v_to = ((P::kRow == 64 ? g >> 1 : g) ^ swizzle(2 * t)) * 16;
+  auto k_piece = [&](int nb, int pc) { return *reinterpret_cast<const uint4*>(k_lane + 8 * nb * P::kRow + (k_to ^ ((pc & 1) * 64)) + (pc >> 1) * 128); };
+  auto v_piece = [&](int mt, int i, int h) {
+    return *reinterpret_cast<const uint4*>(v_lane + (16 * mt + (i & 1) + 8 * (i >> 1)) * P::kRow + (v_to ^ (swizzle(i & 1) * 16)) + h * 128);
+  };
 
   // the lane's part of the query rows of a (sequence, head tile): of head g (and g + 8), laid out as the keys are; fp32 reads them where they are
   uint32_t qr[kF32 ? 1 : NT][kF32 ? 1 : D / 8];
@@ -406,8 +410,10 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   int entry = -1;                                       // the table's entries for the chunk behind it,
   int next_entry = w0 < w1 ? entry_of(next, next_c) : -1;  // and for the next item's
   bool fresh = false;                                   // the item's queries have just been asked for
+  int x = w0 - 1;
+  asm volatile("" : "+r"(x));  // the compiler is not to lay the loop out twice for that round
 #pragma unroll 1
-  for (int x = w0 - 1; x < w1; ++x) {
+  for (; x < w1; ++x) {
     const bool real = x >= w0, more_chunks = x + 1 < w1, ends = !real || c + 1 == item.n;  // of the warp; the item
     const int rows = item.rows;
     int64_t at = -1;
@@ -452,7 +458,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
         for (int pc = 0; pc < NP; ++pc) {
 #pragma unroll
           for (int mt = 0; mt < NG / 2; ++mt) {
-            const uint4 k0 = k_piece(16 * mt + g, 4 * pc + t), k8 = k_piece(16 * mt + 8 + g, 4 * pc + t);
+            const uint4 k0 = k_piece(2 * mt, pc), k8 = k_piece(2 * mt + 1, pc);
             if constexpr (kType == kTypeBf16) {
 #pragma unroll
               for (int e = 0; e < 2; ++e)
@@ -472,27 +478,32 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
       } else {
         // ---------------------------------------------------------------- fp32 scores: 4 lanes per key
         const float* q32 = static_cast<const float*>(a.q) + item.s * a.q_b + (int64_t)item.h0 * a.q_h;
+        uint4 kr[NG][NP];
 #pragma unroll
-        for (int nb = 0; nb < NG; ++nb) {
-          uint4 kr[NP];
+        for (int nb = 0; nb < NG; ++nb)
 #pragma unroll
-          for (int pc = 0; pc < NP; ++pc) kr[pc] = k_piece(8 * nb + g, 4 * pc + t);
+          for (int pc = 0; pc < NP; ++pc) kr[nb][pc] = k_piece(nb, pc);
+#pragma unroll 1
+        for (int r = 0; r < rows; ++r) {
+          float z[NG];
 #pragma unroll
-          for (int r = 0; r < HT; ++r) {
-            if (r < rows) {
-              float z = 0.f;
+          for (int nb = 0; nb < NG; ++nb) z[nb] = 0.f;
 #pragma unroll
-              for (int pc = 0; pc < NP; ++pc) {
-                const float4 qv = __ldg(reinterpret_cast<const float4*>(q32 + r * a.q_h + 16 * pc + 4 * t));
-                z = fmaf(qv.x, __uint_as_float(kr[pc].x), z);
-                z = fmaf(qv.y, __uint_as_float(kr[pc].y), z);
-                z = fmaf(qv.z, __uint_as_float(kr[pc].z), z);
-                z = fmaf(qv.w, __uint_as_float(kr[pc].w), z);
-              }
-              z += __shfl_xor_sync(full, z, 1);
-              z += __shfl_xor_sync(full, z, 2);
-              if (t == 0) weights[warp][8 * nb + g][r] = 8 * nb + g < left ? z * score_scale[0] : -CUDART_INF_F;
+          for (int pc = 0; pc < NP; ++pc) {
+            const float4 qv = __ldg(reinterpret_cast<const float4*>(q32 + r * a.q_h + 16 * pc + 4 * t));
+#pragma unroll
+            for (int nb = 0; nb < NG; ++nb) {
+              z[nb] = fmaf(qv.x, __uint_as_float(kr[nb][pc].x), z[nb]);
+              z[nb] = fmaf(qv.y, __uint_as_float(kr[nb][pc].y), z[nb]);
+              z[nb] = fmaf(qv.z, __uint_as_float(kr[nb][pc].z), z[nb]);
+              z[nb] = fmaf(qv.w, __uint_as_float(kr[nb][pc].w), z[nb]);
             }
+          }
+#pragma unroll
+          for (int nb = 0; nb < NG; ++nb) {
+            z[nb] += __shfl_xor_sync(full, z[nb], 1);
+            z[nb] += __shfl_xor_sync(full, z[nb], 2);
+            if (t == 0) weights[warp][8 * nb + g][r] = 8 * nb + g < left ? z[nb] * score_scale[0] : -CUDART_INF_F;
           }
         }
       }
@@ -583,7 +594,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-              for (int h = 0; h < H2; ++h) u[i][h] = v_piece(16 * mt + 2 * t + (i & 1) + 8 * (i >> 1), 8 * h + g);
+              for (int h = 0; h < H2; ++h) u[i][h] = v_piece(mt, i, h);
             auto pair = [&](int i, int h, int j) {  // element j of the piece, of keys i and i + 1
               return __byte_perm(word(u[i][h], j >> 1), word(u[i + 1][h], j >> 1), j & 1 ? 0x7632 : 0x5410);
             };
@@ -598,7 +609,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
             uint32_t u[4][D / 32];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const uint4 v = v_piece(16 * mt + 2 * t + (i & 1) + 8 * (i >> 1), D == 64 ? g >> 1 : g);
+              const uint4 v = v_piece(mt, i, 0);
 #pragma unroll
               for (int k = 0; k < D / 32; ++k) u[i][k] = D == 64 ? (g & 1 ? word(v, 2 + k) : word(v, k)) : word(v, k);
             }
@@ -652,7 +663,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int in = D == 128 ? i : 2 * i + (lane >> 4);
-          const uint4 vw = v_piece(in, D == 128 ? lane : lane & 15);
+          const uint4 vw = *reinterpret_cast<const uint4*>(queue + 4096 + in * P::kRow + ((D == 128 ? lane : lane & 15) ^ swizzle(in)) * 16);
           const float4 v = make_float4(__uint_as_float(vw.x), __uint_as_float(vw.y), __uint_as_float(vw.z), __uint_as_float(vw.w));
 #pragma unroll
           for (int r4 = 0; r4 < HT / 4; ++r4) {
@@ -767,7 +778,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
       const Item it = part_item[i];
       const int first = part_first[i], rows = it.rows;
       const bool whole = first >= x0 && first + it.n <= x1;
-      float* slot = a.parts + (2 * (int)blockIdx.x + (first < x0 ? 1 : 0)) * P::kSlot;
+      float* slot = a.parts + (2 * (int)blockIdx.x + (first < x0 ? 0 : 1)) * P::kSlot;
 #pragma unroll 1
       for (int row = warp >= turn ? warp - turn : warp - turn + NW; row < rows; row += NW) {
         float top, sum;
@@ -807,23 +818,25 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
     if (!last_arrival) continue;
     // A row by `subs` warps, each with parts sub, sub + subs, ...: 32 of them at a time, a lane for the offset and sum of each.  What the
     // warps come to meets in the shared memory of their second parts.
-    const int subs = max(1, NW / rows);
+    const int subs = rows == 1 ? NW : max(1, (int)((unsigned)NW / (unsigned)rows));
+    const float* const parts = a.parts + 2 * b_first * P::kSlot;
 #pragma unroll 1
     for (int task = warp; task < rows * subs; task += NW) {
-      const int row = task % rows, sub = task / rows;
+      const int sub = (int)((unsigned)task / (unsigned)rows), row = task - sub * rows;
       float top = -CUDART_INF_F, sum = 0.f;
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      auto part_at = [&](int i) { return a.parts + (2 * (b_first + i) + (i ? 1 : 0)) * P::kSlot; };
+      auto part_at = [&](int i) { return parts + max(1, 2 * i) * P::kSlot; };  // the first block's is odd, the others' are even
 #pragma unroll 1
       for (int i0 = sub; i0 < n_parts; i0 += 32 * subs) {
-        const int i = i0 + lane * subs, count = min(32, (n_parts - i0 + subs - 1) / subs);
-        const float mine = lane < count ? __ldcg(part_at(i) + HT * D + row) : -CUDART_INF_F;
-        const float sum_mine = lane < count ? __ldcg(part_at(i) + HT * D + HT + row) : 0.f;
+        const int i = i0 + lane * subs;
+        const bool in = i < n_parts;
+        const float mine = in ? __ldcg(part_at(i) + HT * D + row) : -CUDART_INF_F;
+        const float sum_mine = in ? __ldcg(part_at(i) + HT * D + HT + row) : 0.f;
         float to = mine;
 #pragma unroll
         for (int off = 16; off >= 1; off >>= 1) to = fmaxf(to, __shfl_xor_sync(full, to, off));
         to = fmaxf(to, top);
-        const float alpha = top == to ? 1.f : exp2_approx(top - to), weight = lane < count ? exp2_approx(mine - to) : 0.f;
+        const float alpha = top == to ? 1.f : exp2_approx(top - to), weight = in ? exp2_approx(mine - to) : 0.f;
         top = to;
         float all = sum_mine * weight;
 #pragma unroll
@@ -831,15 +844,17 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
         sum = fmaf(sum, alpha, all);
         o.x *= alpha; o.y *= alpha; o.z *= alpha; o.w *= alpha;
 #pragma unroll 1
-        for (int j = 0; j < count; j += 8) {
+        for (int j = 0; j < 32 && i0 + j * subs < n_parts; j += 8) {
           float4 v[8];
 #pragma unroll
-          for (int u = 0; u < 8; ++u)
-            v[u] = j + u < count ? __ldcg(reinterpret_cast<const float4*>(part_at(i0 + (j + u) * subs) + row * D + 4 * (D == 128 ? lane : lane & 15)))
-                                 : make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int u = 0; u < 8; ++u) {
+            const int k = i0 + (j + u) * subs;
+            v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (k < n_parts) v[u] = __ldcg(reinterpret_cast<const float4*>(part_at(k) + row * D + 4 * (D == 128 ? lane : lane & 15)));
+          }
 #pragma unroll
           for (int u = 0; u < 8; ++u) {
-            const float f = __shfl_sync(full, weight, (j + u) & 31);  // 0 behind the last
+            const float f = __shfl_sync(full, weight, j + u);  // 0 behind the last
             o.x = fmaf(v[u].x, f, o.x); o.y = fmaf(v[u].y, f, o.y); o.z = fmaf(v[u].z, f, o.z); o.w = fmaf(v[u].w, f, o.w);
           }
         }
@@ -855,6 +870,17 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
       float4 o;
       together(of, row, top, sum, o);
       write_row(it, row, top, sum, o);
+    }
+  }
+  // sequences without keys
+#pragma unroll 1
+  for (int s = (int)(blockIdx.x + gridDim.x * warp); s < a.S; s += (int)gridDim.x * NW) {
+    if (length(s) > 0) continue;
+#pragma unroll 1
+    for (int h = 0; h < a.Hq; ++h) {
+      if (a.lse && lane == 0) a.lse[(int64_t)s * a.Hq + h] = -CUDART_INF_F;
+      if (lane < D * (kF32 ? 4 : 2) / 16)
+        reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.out) + (s * a.o_b + h * a.o_h) * (kF32 ? 4 : 2))[lane] = make_uint4(0, 0, 0, 0);
     }
   }
   if (__any_sync(full, bad_page) && lane == 0 && a.status) atomicOr(a.status, TSD_STATUS_BAD_INDEX);
