@@ -645,7 +645,7 @@ typedef struct {
  * a_j = p * inv_freq[j], j < rotary_dim / 2, every pair of dimensions (j, j + rotary_dim / 2), or (2j, 2j + 1)
  * with `interleaved`, of its queries and keys becomes (x cos a - y sin a, x sin a + y cos a); dimensions from
  * rotary_dim on and the values stay as they are.  Angles are taken in fp64, products in fp32; each result is
- * rounded once, to the type it is stored in (TSD_E4M3: rn(x / scale), saturating at 448).
+ * rounded once, to the type it is stored in (TSD_E4M3: x times the fp32 reciprocal of scale, saturating at 448).
  *
  *   cache        nullable: rotate only (then k_out, or q and q_out, take the results; v is not read).
  *   k, v         device [batch, n_blocks * n_rows, n_kv_heads, head_dim] of `dtype`, strides kv_stride (batch,

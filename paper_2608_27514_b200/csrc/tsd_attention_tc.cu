@@ -71,6 +71,16 @@ constexpr int kKeys = 64;                      // keys per tile
 constexpr int kMaxItems = 256;                 // work items of one block (what the warps need to know of them sits in shared memory)
 constexpr uint32_t kSub = 16384;               // bytes of one [128 rows x 64 elements] bf16 sub-tile
 constexpr uint32_t kSubKV = 8192;              // bytes of one [64 keys x 64 elements] bf16 sub-tile
+// Where the cached keys come from: one dense cache per sequence, or pages of 2^page_shift rows.
+struct TcDense {
+  static constexpr bool kPaged = false;
+};
+struct TcPages {
+  static constexpr bool kPaged = true;
+  const int32_t* table;
+  int64_t table_stride;
+  int page_shift, n_pages;
+};
 // Shared-memory layout for a head_dim of D = 64 or 128 (one sub-tile per 64 elements of head_dim).
 template <int D>
 struct TcSmem {
@@ -87,7 +97,9 @@ struct TcSmem {
   static constexpr uint32_t kOffLpart = kOffMref + 1024;
   static constexpr uint32_t kOffMpart = kOffLpart + 3 * 3 * 128 * 4;
   static constexpr uint32_t kOffItems = kOffMpart + 3 * 3 * 128 * 4;  // key tiles / cache length / mask record / sequence and kv head per item
-  static constexpr uint32_t kBytes = kOffItems + 4 * kMaxItems * 4 + 1024;  // + slack to align the base to 1 KB
+  static constexpr uint32_t kOffPages = kOffItems + 4 * kMaxItems * 4;  // over pages: 32 page indices each for the K and the V producer
+  template <typename Cache>
+  static constexpr uint32_t kBytesFor = kOffPages + (Cache::kPaged ? 256 : 0) + 1024;  // + slack to align the base to 1 KB
 };
 static_assert(kKeys == kKeyTile, "the mask blob lists tiles of this many keys");
 // Tensor-memory columns.  At head_dim 128 everything is in use and P is one bf16 per score.  At head_dim 64
@@ -372,16 +384,18 @@ struct TcParams {
   __nv_bfloat16* out;             // where cut items are written without a tensor map
   int64_t os_b, os_r, os_h;
 };
-// Where the cached keys come from: one dense cache per sequence, or pages of 2^page_shift rows.
-struct TcDense {
-  static constexpr bool kPaged = false;
-};
-struct TcPages {
-  static constexpr bool kPaged = true;
-  const int32_t* table;
-  int64_t table_stride;
-  int page_shift, n_pages;
-};
+// The copies of a tile of 64 keys from N pages; lane (tile in its set) * N + i has the i-th one's index.
+template <int D, int N>
+__device__ __forceinline__ void paged_copies(uint32_t dst, uint32_t step, const CUtensorMap* map, uint32_t bar, int g, int page, int in_set) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int where = __shfl_sync(0xffffffffu, page, in_set * N + i);
+    if (elect_one()) {
+      tma_load_4d(dst + (uint32_t)i * step, map, bar, 0, g, 0, where);
+      if (D == 128) tma_load_4d(dst + kSubKV + (uint32_t)i * step, map, bar, 64, g, 0, where);
+    }
+  }
+}
 
 // The MMAs of a tile go out as ONE block of instructions: the issuing lane shares its scheduler with
 // three softmax warps, so every instruction between two MMAs (a predicate, a 64-bit add for a
@@ -684,9 +698,13 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     // thread needs several hundred clocks per tile for its waits and copies, and K must run up to
     // four tiles ahead of V.
     if constexpr (kPaged) {
-      // A cached tile is a copy per page that it touches (per 64 rows of a larger one), the page its outermost coordinate: lane i sees to
-      // the tile's i-th copy.  The lanes look up 32 entries at a time, of the tiles to come, and a whole set before it is needed: the way
-      // to L2 takes as long as a tile.
+      // A cached tile is a copy per page that it touches (per 64 rows of a larger one), the page its outermost coordinate.  The lanes look
+      // up 32 entries at a time, of the tiles to come, and a whole set before it is needed: the way to L2 takes as long as a tile.  With one
+      // copy per tile lane 0 goes through a set by itself, the pages in shared memory, as over a dense cache; with more the whole warp walks
+      // the tiles and hands the pages on by shuffles, the copies of a tile laid out in a row.  These warps share their schedulers with
+      // the softmax, so every instruction per tile counts: 896 items, dense 211 us, over pages of 64 / 32 / 16 / 8 rows 213 / 233 / 255 / 313; a
+      // lone lane with a lookup per copy 346 / 423 / 572 / 889, a lane per copy 216 / 260 / 317 / 423, lane 0 in a loop over the copies
+      // 275 / 310 / 414 / 609.
       // Only what holds rows below the cache length is looked up; behind it a page may not have been handed out.  The copy engine fills what lies
       // outside the pool with zeros, and so it does for an entry that is no page of the pool, which is reported.
       const bool is_k = warp == kKProducerWarp;
@@ -727,10 +745,70 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       };
       auto first_entries = [&](int it, int j) { return entries(item_sg[it] / p.Hkv, item_clen[it], j); };
       const int j0 = kCut ? *tile_first : 0;
+      auto page_in_pool = [&](int page) { return page >= 0 && page < pages.n_pages; };
       int now = -1, ahead = n_run > 0 ? first_entries(0, j0) : -1;  // the set at hand, the one behind it
       bool missing = false;
       int G = 0, b = 0;
       uint32_t ph = 0;
+      if (n_box == 1) {
+        volatile int32_t* set_pages = reinterpret_cast<volatile int32_t*>(base_ptr + L::kOffPages) + (is_k ? 0 : 32);
+        auto issue_q_alone = [&](bool block) {
+          if (!ok || q_issued >= n_run) return;
+          const int x = q_issued;
+          const uint32_t b = bar(QT_READY + ((x - 1) & 1)), ph = ((x - 1) >> 1) & 1;
+          if (block) ok = mbar_wait(b, ph, abort_flag, 100);
+          else if (!mbar_test_wait(b, ph)) return;
+          if (!ok) return;
+          int s, h, qt;
+          item_coords(x, s, h, qt);
+          mbar_expect_tx(bar(QS_FULL), kTileBytes);
+          tma_load_4d(base + kOffQ, &map_q, bar(QS_FULL), 0, h, qt * kTile, s);
+          if (D == 128) tma_load_4d(base + kOffQ + kSub, &map_q, bar(QS_FULL), 64, h, qt * kTile, s);
+          q_issued = x + 1;
+        };
+        for (int it = 0; it < n_run && ok; ++it) {
+          const int clen = item_clen[it];
+          const int s = item_sg[it] / p.Hkv, g = item_sg[it] - s * p.Hkv, n_ct = (clen + kKeys - 1) / kKeys, end = j0 + item_T[it];
+          const int cached_end = min(max(n_ct, j0), end);
+          const int32_t* rec = mask + item_rec[it];
+          if (n_ct <= j0 && it + 1 < n_run) ahead = first_entries(it + 1, 0);
+          for (int set0 = j0; set0 < end && ok;) {
+            const int set_end = min(set0 + 32, cached_end), last = set_end == cached_end ? end : set_end;  // the draft tiles follow the last set
+            if (set0 < cached_end) {
+              missing |= set0 + lane < set_end && !page_in_pool(ahead);
+              set_pages[lane] = page_in_pool(ahead) ? ahead : -1;
+              if (set_end < cached_end) ahead = entries(s, clen, set_end);
+              else if (it + 1 < n_run) ahead = first_entries(it + 1, 0);
+            }
+            __syncwarp();
+            if (lane == 0) {
+              while (is_k && ok && q_issued <= it) issue_q_alone(true);
+              for (int j = set0; j < last && ok; ++j, ++G) {
+                if (is_k) issue_q_alone(false);
+                if (!ok) break;
+                if (G >= n_stage) ok = mbar_wait(bar(free0 + b), ph ^ 1u, abort_flag, 100);
+                if (!ok) break;
+                const bool cached = j < n_ct;
+                const int row = cached ? (j * kKeys) & ((1 << pages.page_shift) - 1) : rec[2 + 2 * (j - n_ct)] * kKeys;
+                const int where = cached ? set_pages[j - set0] : s;
+                const CUtensorMap* m = cached ? mc : md;
+                const uint32_t dst = stage0 + b * kKVBytes, full_bar = bar(full0 + b);
+                mbar_expect_tx(full_bar, kKVBytes);
+                if (is_k && G < kNSb) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], 4;" ::"r"(full_bar) : "memory");
+                tma_load_4d(dst, m, full_bar, 0, g, row, where);
+                if (D == 128) tma_load_4d(dst + kSubKV, m, full_bar, 64, g, row, where);
+                issued = G + 1;
+                if (++b == n_stage) { b = 0; ph ^= 1u; }
+              }
+            }
+            ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+            set0 = last;
+          }
+        }
+        // what lane 0 has issued, for the drain below
+        issued = __shfl_sync(0xffffffffu, issued, 0);
+        q_issued = __shfl_sync(0xffffffffu, q_issued, 0);
+      } else
       for (int it = 0; it < n_run && ok; ++it) {
         while (is_k && ok && q_issued <= it) issue_q(true);
         const int clen = item_clen[it];
@@ -752,21 +830,18 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
           }
           __syncwarp();
           if (j < n_ct) {
-            const int in_set = (j - j0) % set;
+            const int in_set = (j - j0) & (set - 1);
             if (in_set == 0) {
-              now = ahead;
+              const bool there = page_in_pool(ahead);
+              missing |= j * kKeys + lane * box < clen && !there;
+              now = there ? ahead : -1;
               if (j + set < min(n_ct, j0 + T)) ahead = entries(s, clen, j + set);
               else if (it + 1 < n_run) ahead = first_entries(it + 1, 0);
             }
-            int page = __shfl_sync(0xffffffffu, now, in_set * n_box + lane);
-            if (lane < n_box) {
-              const int key = j * kKeys + lane * box, in_page = key & ((1 << pages.page_shift) - 1);
-              const bool there = page >= 0 && page < pages.n_pages;
-              missing |= key < clen && !there;
-              if (!there) page = -1;
-              tma_load_4d(dst + (uint32_t)(lane * box) * 128u, mc, full_bar, 0, g, in_page, page);
-              if (D == 128) tma_load_4d(dst + kSubKV + (uint32_t)(lane * box) * 128u, mc, full_bar, 64, g, in_page, page);
-            }
+            const uint32_t row_bytes = (uint32_t)box * 128u;
+            if (n_box == 2) paged_copies<D, 2>(dst, row_bytes, mc, full_bar, g, now, in_set);
+            else if (n_box == 4) paged_copies<D, 4>(dst, row_bytes, mc, full_bar, g, now, in_set);
+            else paged_copies<D, 8>(dst, row_bytes, mc, full_bar, g, now, in_set);
           } else if (lane == 0) {
             const int row = rec[2 + 2 * (j - n_ct)] * kKeys;
             tma_load_4d(dst, md, full_bar, 0, g, row, s);
@@ -1497,9 +1572,9 @@ static cudaError_t allow_smem(int dev) {
   static bool done[kMaxDevices];
   std::lock_guard<std::mutex> lock(mu);
   if (done[dev]) return cudaSuccess;
-  cudaError_t e = cudaFuncSetAttribute(attention_tc_kernel<D, false, Cache>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcSmem<D>::kBytes);
+  cudaError_t e = cudaFuncSetAttribute(attention_tc_kernel<D, false, Cache>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcSmem<D>::template kBytesFor<Cache>);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(attention_tc_kernel<D, true, Cache>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcSmem<D>::kBytes);
+    e = cudaFuncSetAttribute(attention_tc_kernel<D, true, Cache>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcSmem<D>::template kBytesFor<Cache>);
   done[dev] = e == cudaSuccess;
   return e;
 }
@@ -1527,7 +1602,7 @@ static int cut_items(int64_t n_items, int T) {
       cudaLaunchConfig_t cfg = {};
       cfg.gridDim = dim3((unsigned)n * 64);
       cfg.blockDim = dim3(kTcThreads);
-      cfg.dynamicSmemBytes = TcSmem<D>::kBytes;
+      cfg.dynamicSmemBytes = TcSmem<D>::template kBytesFor<TcDense>;
       cfg.attrs = &attr;
       cfg.numAttrs = 1;
       int found = 0;
@@ -1609,7 +1684,7 @@ static int launch_tc(const AttnArgs& a) {
   Cache pages;
   if constexpr (kPaged) pages = TcPages{a.pages->table, a.pages->table_stride, a.pages->shift, a.pages->n_pages};
   if (p.cut > 1) {
-    cudaError_t e = launch_clusters(p.cut, attention_tc_kernel<D, true, Cache>, (unsigned)(n_items * p.cut), kTcThreads, TcSmem<D>::kBytes, a.stream,
+    cudaError_t e = launch_clusters(p.cut, attention_tc_kernel<D, true, Cache>, (unsigned)(n_items * p.cut), kTcThreads, TcSmem<D>::template kBytesFor<Cache>, a.stream,
                                     mq, mkc, mvc, mkd, mvd, mo, p, pages);
     return e != cudaSuccess ? cuda_fail(e, "attention_tc_kernel") : TSD_OK;
   }
@@ -1618,7 +1693,7 @@ static int launch_tc(const AttnArgs& a) {
   // items of 8 tiles on 148 SMs: 1.56 and 2.71-2.83 ms; in whole rounds 1.56 and 1.59).
   const int64_t sms = std::max(device_facts().sms, 1);
   const int64_t grid = std::min(n_items, sms * ((n_items + sms * kMaxItems - 1) / (sms * kMaxItems)));
-  cudaError_t e = launch(attention_tc_kernel<D, false, Cache>, (unsigned)grid, kTcThreads, TcSmem<D>::kBytes, a.stream, mq, mkc, mvc, mkd,
+  cudaError_t e = launch(attention_tc_kernel<D, false, Cache>, (unsigned)grid, kTcThreads, TcSmem<D>::template kBytesFor<Cache>, a.stream, mq, mkc, mvc, mkd,
                          mvd, mo, p, pages);
   if (e != cudaSuccess) return cuda_fail(e, "attention_tc_kernel");
   return TSD_OK;

@@ -1,10 +1,10 @@
 // New rows into a paged K/V cache, with the position rotation on the way (paper App. A: the dual cache is refreshed at block
 // boundaries; a paged cache has no counterpart there).
 //
-// One block per new row.  Its angles, position x inverse frequency, are taken once for all heads: reduced in fp64 to an eighth of
-// a turn around the nearest quarter (a position of 10^6 leaves 1e-10 of an angle there; in fp32 it would leave 0.1), then sine and cosine
-// in fp32, left in shared memory.  Then every thread moves units of 16 dimensions of a head: the two chunks of 8 that rotate
-// into each other, or 16 neighbours.  The loads of a batch of units are issued before the angles are waited for.
+// A block takes a row, or several where a row has few heads.  A row's angles, position x inverse frequency, are taken once for all heads: reduced in
+// fp64 to an eighth of a turn around the nearest quarter (a position of 10^6 leaves 1e-10 of an angle there; in fp32 it would leave 0.1),
+// then sine and cosine in fp32, left in shared memory.  Every thread moves units of 16 dimensions of a head: the two chunks of 8 that
+// rotate into each other, or 16 neighbours.  The loads of a batch of units are issued before the angles and the page are looked up.
 // Bound by memory: each row is read once and written once, and nothing but the tables comes on top.
 #include <cuda_fp8.h>
 #include <algorithm>
@@ -46,10 +46,13 @@ PagedView paged_view(const tsd_paged_cache& c) {
 
 constexpr int kAppendThreads = 256;
 constexpr int kAppendUnits = 3;   // units of a thread in flight: a row of 32 heads each of queries, keys and values is one batch
+constexpr int kAppendBlocks = 4;  // per SM
+constexpr int kAppendRows = 8;    // rows of a block at most
 
 struct AppendParams {
   PagedView cache;
   bool cached;
+  int rows, rows_per_block;       // of all sequences
   int n_blocks, n_rows, Hq, Hkv;  // Hq = 0: no queries
   const int32_t *block, *n_new, *first_slot, *positions;
   const float* inv_freq;
@@ -89,15 +92,16 @@ __device__ __forceinline__ void store_chunk(__nv_bfloat16* p, const float (&x)[8
   }
   *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
 }
-// into a page: the model's type, or e4m3 of x / scale (a correctly rounded quotient, then one rounding to 8 bits)
+// into a page: the model's type, or e4m3 of x times the scale's reciprocal (an ulp of fp32 beside x / scale; eight divisions a chunk
+// would be more work than all the rest)
 __device__ __forceinline__ void store_cached(float* p, const float (&x)[8], float) { store_chunk(p, x); }
 __device__ __forceinline__ void store_cached(__nv_bfloat16* p, const float (&x)[8], float) { store_chunk(p, x); }
-__device__ __forceinline__ void store_cached(uint8_t* p, const float (&x)[8], float scale) {
+__device__ __forceinline__ void store_cached(uint8_t* p, const float (&x)[8], float unit) {
   uint32_t u[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * i] / scale, x[4 * i + 1] / scale), __NV_SATFINITE, __NV_E4M3);
-    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * i + 2] / scale, x[4 * i + 3] / scale), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * i] * unit, x[4 * i + 1] * unit), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * i + 2] * unit, x[4 * i + 3] * unit), __NV_SATFINITE, __NV_E4M3);
     u[i] = lo | hi << 16;
   }
   *reinterpret_cast<uint2*>(p) = make_uint2(u[0], u[1]);
@@ -117,72 +121,97 @@ __device__ __forceinline__ float2 cos_sin(int position, float inv_freq) {
   return make_float2(turn == 1 || turn == 2 ? -cx : cx, turn >= 2 ? -sx : sx);
 }
 
-template <typename T, typename C, int D, bool kNext>  // kNext: neighbouring dimensions (2j, 2j + 1) form the pairs
-__global__ void __launch_bounds__(kAppendThreads)
+// kNext: neighbouring dimensions (2j, 2j + 1) form the pairs.  kOne: one row per block; every thread looks up by itself whose it is, without a barrier.
+template <typename T, typename C, int D, bool kNext, bool kOne>
+__global__ void __launch_bounds__(kAppendThreads, kAppendBlocks)
 append_kernel(const T* k, const T* v, const T* q, T* k_out, T* q_out, AppendParams p) {
-  __shared__ float2 turns[D / 2];
+  struct Row {
+    int s, from, slot;  // sequence, row of k, v and q (-1: does not count, -2: its block does not exist), slot in the cache
+    bool in_cache;      // it is one
+  };
+  constexpr int kRows = kOne ? 1 : kAppendRows;
+  __shared__ float2 turns[kRows][D / 2];
+  __shared__ Row rows[kRows];
+  __shared__ int64_t row_at[kRows];  // where the row's page has it, in elements; -1: nowhere
   grid_wait(k, v, q, k_out, q_out);
   settle(p.block, p.n_new, p.first_slot, p.positions, p.inv_freq, p.cache.table, p.cache.k_scale, p.cache.v_scale);
-  const int tid = threadIdx.x;
-  const int64_t s = blockIdx.x / (unsigned)p.n_rows;
-  const int i = (int)(blockIdx.x % (unsigned)p.n_rows);
-  const int n_new = p.n_new ? min(p.n_new[s], p.n_rows) : p.n_rows;
-  const int block = p.block ? p.block[s] : 0;
-  const int64_t slot = (int64_t)(p.first_slot ? p.first_slot[s] : 0) + i;
-  if (i >= n_new) return;
-  if (block < 0 || block >= p.n_blocks) {
-    if (tid == 0 && p.status) atomicOr(p.status, TSD_STATUS_BAD_INDEX);
-    return;
+  const int tid = threadIdx.x, first = (int)blockIdx.x * (kOne ? 1 : p.rows_per_block), count = kOne ? 1 : min(p.rows_per_block, p.rows - first);
+  auto look_up = [&](int f) {
+    const int s = (int)((unsigned)f / (unsigned)p.n_rows), i = f - s * p.n_rows;
+    const int n_new = p.n_new ? p.n_new[s] : p.n_rows, block = p.block ? p.block[s] : 0;
+    const int64_t slot = (int64_t)(p.first_slot ? p.first_slot[s] : 0) + i;
+    const bool there = block >= 0 && block < p.n_blocks;
+    return Row{s, i >= n_new ? -1 : there ? block * p.n_rows + i : -2, (int)slot, slot >= 0 && slot < p.cache.cap};
+  };
+  Row only;
+  if (kOne) {
+    only = look_up(first);
+    if (only.from == -1) return;
+  } else {
+    if (tid < count) rows[tid] = look_up(first + tid);
+    __syncthreads();
   }
-  const int page = p.cached && slot >= 0 && slot < p.cache.cap ? page_of(p.cache, s, (int)slot) : -1;
-  if (tid < p.rot / 2) {
-    const int position = p.positions ? p.positions[s * p.n_rows + i] : (int)slot;
-    turns[tid] = cos_sin(position, p.inv_freq[tid]);
-  }
-  const int64_t row = (int64_t)block * p.n_rows + i;
-  const int64_t at = page < 0 ? 0 : (int64_t)page * p.cache.ps_p + (slot & ((1 << p.cache.shift) - 1)) * p.cache.ps_r;
-  C* const k_page = const_cast<C*>(static_cast<const C*>(p.cache.k)) + at;
-  C* const v_page = const_cast<C*>(static_cast<const C*>(p.cache.v)) + at;
+  auto row_of = [&](int r) -> const Row& { return kOne ? only : rows[r]; };
 
-  // Units of 16 dimensions: heads of q, then of k, then of v; D / 16 per head.  A thread's units have the same place in their heads.
-  constexpr int kPer = D / 16;
+  // Units of 16 dimensions: heads of q, then of k, then of v, row by row; D / 16 per head.  A thread's units have the same place in their heads.
+  constexpr int kPer = D / 16, kStep = kAppendThreads / kPer;
   static_assert(kAppendThreads % kPer == 0, "a thread's place in a head stays the same");
   const int place = tid % kPer, half = p.rot / 2;
   const bool turning = place * 16 < p.rot;
   // the unit's two chunks of 8: dimensions [d0, d0 + 8) and [d1, d1 + 8)
   const int d0_rot = kNext || !turning ? place * 16 : place * 8, d1_rot = kNext || !turning ? place * 16 + 8 : half + place * 8;
-  const int n_heads = p.Hq + p.Hkv + (p.cached ? p.Hkv : 0);
+  const int heads = p.Hq + p.Hkv + (p.cached ? p.Hkv : 0);
+  int row = 0, head = tid / kPer;  // of the thread's next unit
   bool waited = false;
-  for (int h0 = tid / kPer; h0 < n_heads || !waited; h0 += kAppendUnits * (kAppendThreads / kPer)) {
+  do {
     decltype(load_chunk(k)) raw[kAppendUnits][2];
+    int row0 = row, head0 = head;
 #pragma unroll
-    for (int u = 0; u < kAppendUnits; ++u) {
-      const int h = h0 + u * (kAppendThreads / kPer);
-      if (h >= n_heads) continue;
-      const T* src = h < p.Hq ? q + s * p.q_b + row * p.q_r + h * p.q_h
-                              : (h < p.Hq + p.Hkv ? k + (h - p.Hq) * p.kv_h : v + (h - p.Hq - p.Hkv) * p.kv_h) + s * p.kv_b + row * p.kv_r;
-      const bool is_v = h >= p.Hq + p.Hkv;  // values do not turn
+    for (int u = 0; u < kAppendUnits; ++u, head += kStep) {
+      while (head >= heads && row < count) { head -= heads; ++row; }
+      if (row >= count || row_of(row).from < 0) continue;
+      const int64_t s = row_of(row).s, from = row_of(row).from;
+      const T* src = head < p.Hq ? q + s * p.q_b + from * p.q_r + head * p.q_h
+                                 : (head < p.Hq + p.Hkv ? k + (head - p.Hq) * p.kv_h : v + (head - p.Hq - p.Hkv) * p.kv_h) + s * p.kv_b + from * p.kv_r;
+      const bool is_v = head >= p.Hq + p.Hkv;  // values do not turn
       raw[u][0] = load_chunk(src + (is_v ? place * 16 : d0_rot));
       raw[u][1] = load_chunk(src + (is_v ? place * 16 + 8 : d1_rot));
     }
     if (!waited) {
+      for (int e = tid; e < count * half; e += kAppendThreads) {
+        const int r = kOne ? 0 : (int)((unsigned)e / (unsigned)half), j = e - r * half, f = first + r;
+        if (row_of(r).from >= 0) turns[r][j] = cos_sin(p.positions ? p.positions[f] : row_of(r).slot, p.inv_freq[j]);
+      }
+      if (tid < count) {
+        int64_t at = -1;
+        const Row& mine = row_of(tid);
+        bool missing = mine.from == -2;
+        if (p.cached && mine.from >= 0) {
+          const int page = mine.in_cache ? page_of(p.cache, mine.s, mine.slot) : -1;
+          if (page >= 0) at = (int64_t)page * p.cache.ps_p + (mine.slot & ((1 << p.cache.shift) - 1)) * p.cache.ps_r;
+          else missing = true;
+        }
+        if (missing && p.status) atomicOr(p.status, TSD_STATUS_BAD_INDEX);
+        row_at[tid] = at;
+      }
       __syncthreads();
       waited = true;
     }
 #pragma unroll
-    for (int u = 0; u < kAppendUnits; ++u) {
-      const int h = h0 + u * (kAppendThreads / kPer);
-      if (h >= n_heads) continue;
+    for (int u = 0; u < kAppendUnits; ++u, head0 += kStep) {
+      while (head0 >= heads && row0 < count) { head0 -= heads; ++row0; }
+      if (row0 >= count || row_of(row0).from < 0) continue;
       float x[8], y[8];
       widen(raw[u][0], x);
       widen(raw[u][1], y);
-      const bool is_v = h >= p.Hq + p.Hkv;
+      const bool is_v = head0 >= p.Hq + p.Hkv;
       const int d0 = is_v ? place * 16 : d0_rot, d1 = is_v ? place * 16 + 8 : d1_rot;
       if (turning && !is_v) {
+        const float2* turn = turns[row0] + place * 8;
         if (kNext) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float2 a = turns[place * 8 + j], b = turns[place * 8 + 4 + j];
+            const float2 a = turn[j], b = turn[4 + j];
             const float x0 = x[2 * j], x1 = x[2 * j + 1], y0 = y[2 * j], y1 = y[2 * j + 1];
             x[2 * j] = x0 * a.x - x1 * a.y;
             x[2 * j + 1] = x0 * a.y + x1 * a.x;
@@ -192,43 +221,50 @@ append_kernel(const T* k, const T* v, const T* q, T* k_out, T* q_out, AppendPara
         } else {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const float2 a = turns[place * 8 + j];
+            const float2 a = turn[j];
             const float x0 = x[j], y0 = y[j];
             x[j] = x0 * a.x - y0 * a.y;
             y[j] = x0 * a.y + y0 * a.x;
           }
         }
       }
-      if (h < p.Hq) {
-        T* dst = q_out + s * p.qo_b + row * p.qo_r + h * p.qo_h;
+      const int64_t s = row_of(row0).s, from = row_of(row0).from;
+      if (head0 < p.Hq) {
+        T* dst = q_out + s * p.qo_b + from * p.qo_r + head0 * p.qo_h;
         store_chunk(dst + d0, x);
         store_chunk(dst + d1, y);
         continue;
       }
-      const int g = h - p.Hq - (is_v ? p.Hkv : 0);
+      const int g = head0 - p.Hq - (is_v ? p.Hkv : 0);
       if (!is_v && k_out) {
-        T* dst = k_out + s * p.ko_b + row * p.ko_r + g * p.ko_h;
+        T* dst = k_out + s * p.ko_b + from * p.ko_r + g * p.ko_h;
         store_chunk(dst + d0, x);
         store_chunk(dst + d1, y);
       }
-      if (page >= 0) {
+      const int64_t at = row_at[row0];
+      if (at >= 0) {
         const float* scales = is_v ? p.cache.v_scale : p.cache.k_scale;
-        const float scale = scales ? scales[g] : 1.f;
-        C* dst = (is_v ? v_page : k_page) + g * p.cache.ps_h;
-        store_cached(dst + d0, x, scale);
-        store_cached(dst + d1, y, scale);
+        const float unit = sizeof(C) == 1 && scales ? 1.f / scales[g] : 1.f;
+        C* dst = const_cast<C*>(static_cast<const C*>(is_v ? p.cache.v : p.cache.k)) + at + g * p.cache.ps_h;
+        store_cached(dst + d0, x, unit);
+        store_cached(dst + d1, y, unit);
       }
     }
-  }
-  if (p.cached && page < 0 && tid == 0 && p.status) atomicOr(p.status, TSD_STATUS_BAD_INDEX);
+  } while (row < count);
 }
 
+template <typename T, typename C, int D>
+static cudaError_t launch_append(const tsd_append_args& a, const AppendParams& p, cudaStream_t stream) {
+  const bool one = p.rows_per_block == 1;
+  const auto kernel = a.interleaved ? (one ? append_kernel<T, C, D, true, true> : append_kernel<T, C, D, true, false>)
+                                    : (one ? append_kernel<T, C, D, false, true> : append_kernel<T, C, D, false, false>);
+  return launch(kernel, dim3((unsigned)((p.rows + p.rows_per_block - 1) / p.rows_per_block)), dim3(kAppendThreads), 0, stream,
+                static_cast<const T*>(a.k), static_cast<const T*>(a.v), static_cast<const T*>(a.q), static_cast<T*>(a.k_out),
+                static_cast<T*>(a.q_out), p);
+}
 template <typename T, typename C>
 static cudaError_t launch_append(const tsd_append_args& a, const AppendParams& p, cudaStream_t stream) {
-  const auto kernel = a.head_dim == 64 ? (a.interleaved ? append_kernel<T, C, 64, true> : append_kernel<T, C, 64, false>)
-                                       : (a.interleaved ? append_kernel<T, C, 128, true> : append_kernel<T, C, 128, false>);
-  return launch(kernel, dim3((unsigned)((int64_t)a.batch * a.n_rows)), dim3(kAppendThreads), 0, stream, static_cast<const T*>(a.k),
-                static_cast<const T*>(a.v), static_cast<const T*>(a.q), static_cast<T*>(a.k_out), static_cast<T*>(a.q_out), p);
+  return a.head_dim == 64 ? launch_append<T, C, 64>(a, p, stream) : launch_append<T, C, 128>(a, p, stream);
 }
 
 // Strides (batch, row, head) of rows of heads; a dimension of size 1 may have any.
@@ -279,10 +315,14 @@ extern "C" int tsd_append_paged_kv(const tsd_append_args* args, tsd_stream_t str
   p.cached = a.cache != nullptr;
   if (p.cached) p.cache = tsd::paged_view(*a.cache);
   p.n_blocks = a.n_blocks; p.n_rows = a.n_rows;
+  p.rows = a.batch * a.n_rows;
   p.Hq = a.q ? a.n_q_heads : 0; p.Hkv = a.n_kv_heads;
   p.block = a.block; p.n_new = a.n_new; p.first_slot = a.first_slot; p.positions = a.positions;
   p.inv_freq = a.inv_freq;
   p.rot = a.rotary_dim;
+  // as many rows to a block as make one batch of units, if that leaves every SM its four blocks
+  const int units = (p.Hq + p.Hkv * (p.cached ? 2 : 1)) * (a.head_dim / 16);
+  p.rows_per_block = std::max(1, std::min({tsd::kAppendRows, tsd::kAppendThreads * tsd::kAppendUnits / units, p.rows / (tsd::kAppendBlocks * tsd::kPlanSms)}));
   p.kv_b = a.kv_stride[0]; p.kv_r = a.kv_stride[1]; p.kv_h = a.kv_stride[2];
   p.q_b = a.q_stride[0]; p.q_r = a.q_stride[1]; p.q_h = a.q_stride[2];
   p.ko_b = a.k_out_stride[0]; p.ko_r = a.k_out_stride[1]; p.ko_h = a.k_out_stride[2];
