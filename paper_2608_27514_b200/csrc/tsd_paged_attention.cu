@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   __shared__ Item part_item[2 * NW];                          // whose (n = 0: no part)
   __shared__ int part_first[2 * NW];                          // its first chunk
   __shared__ __align__(16) float weights[kF32 ? NW : 1][kF32 ? KC : 1][HT];
-  __shared__ int last_arrival;
+  __shared__ int last_arrival[2];
   static_assert(2 * NW <= 32, "a lane per part");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   constexpr unsigned full = 0xffffffffu;
@@ -791,8 +791,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
           if (lane == 0) { slot[HT * D + row] = top; slot[HT * D + HT + row] = sum; }
         }
       }
-      turn += rows;
-      if (turn >= NW) turn -= NW;
+      turn = (turn + rows) % NW;
       if (!whole) {
         if (n_shared == 0) shared0 = i;
         else shared1 = i;
@@ -800,76 +799,95 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
       }
     }
   }
-  // An item of several blocks: the last of them to arrive puts its parts together.  (The barrier puts the block's writes before
-  // the arrival, whose release and acquire take them to the block that arrives last.)
-#pragma unroll 1
-  for (int k = 0; k < n_shared; ++k) {
-    const int i0 = k == 0 ? shared0 : shared1;
-    const Item it = part_item[i0];
-    const int first = part_first[i0], rows = it.rows, b_first = block_of(first), n_parts = block_of(first + it.n - 1) - b_first + 1;
+  // An item of several blocks: the last of them to arrive puts its parts together.  The barrier puts the block's writes before
+  // the arrivals, whose release and acquire take them to the block that arrives last.
+  if (n_shared > 0) {
     __syncthreads();
-    if (tid == 0) {
+    if (warp < n_shared && lane == 0) {
+      const int i0 = warp == 0 ? shared0 : shared1, b_first = block_of(part_first[i0]);
+      const int n_parts = block_of(part_first[i0] + part_item[i0].n - 1) - b_first + 1;
       unsigned before;
       asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.tickets + b_first) : "memory");
-      last_arrival = before + 1 == (unsigned)n_parts;
-      if (last_arrival) a.tickets[b_first] = 0;
+      const bool last = before + 1 == (unsigned)n_parts;
+      last_arrival[warp] = last;
+      if (last) a.tickets[b_first] = 0;
     }
     __syncthreads();
-    if (!last_arrival) continue;
-    // A row by `subs` warps, each with parts sub, sub + subs, ...: 32 of them at a time, a lane for the offset and sum of each.  What the
-    // warps come to meets in the shared memory of their second parts.
-    const int subs = rows == 1 ? NW : max(1, (int)((unsigned)NW / (unsigned)rows));
-    const float* const parts = a.parts + 2 * b_first * P::kSlot;
 #pragma unroll 1
-    for (int task = warp; task < rows * subs; task += NW) {
-      const int sub = (int)((unsigned)task / (unsigned)rows), row = task - sub * rows;
-      float top = -CUDART_INF_F, sum = 0.f;
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      auto part_at = [&](int i) { return parts + max(1, 2 * i) * P::kSlot; };  // the first block's is odd, the others' are even
+    for (int k = 0; k < n_shared; ++k) {
+      if (!last_arrival[k]) continue;
+      const int i0 = k == 0 ? shared0 : shared1;
+      const Item it = part_item[i0];
+      const int first = part_first[i0], rows = it.rows, b_first = block_of(first), n_parts = block_of(first + it.n - 1) - b_first + 1;
+      // A row by one warp; many parts, and warps to spare: by `subs` warps, each with parts sub, sub + subs, ... , and what they come
+      // to meets in the shared memory of their second parts.  32 parts at a time, a lane for the offset and sum of each.
+      const int subs = n_parts <= 32 ? 1 : max(1, (int)((unsigned)NW / (unsigned)rows));
+      const float* const parts = a.parts + 2 * b_first * P::kSlot;
 #pragma unroll 1
-      for (int i0 = sub; i0 < n_parts; i0 += 32 * subs) {
-        const int i = i0 + lane * subs;
-        const bool in = i < n_parts;
-        const float mine = in ? __ldcg(part_at(i) + HT * D + row) : -CUDART_INF_F;
-        const float sum_mine = in ? __ldcg(part_at(i) + HT * D + HT + row) : 0.f;
-        float to = mine;
-#pragma unroll
-        for (int off = 16; off >= 1; off >>= 1) to = fmaxf(to, __shfl_xor_sync(full, to, off));
-        to = fmaxf(to, top);
-        const float alpha = top == to ? 1.f : exp2_approx(top - to), weight = in ? exp2_approx(mine - to) : 0.f;
-        top = to;
-        float all = sum_mine * weight;
-#pragma unroll
-        for (int off = 16; off >= 1; off >>= 1) all += __shfl_xor_sync(full, all, off);
-        sum = fmaf(sum, alpha, all);
-        o.x *= alpha; o.y *= alpha; o.z *= alpha; o.w *= alpha;
+      for (int task = warp; task < rows * subs; task += NW) {
+        const int sub = (int)((unsigned)task / (unsigned)rows), row = task - sub * rows;
+        float top = -CUDART_INF_F, sum = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto part_at = [&](int i) { return parts + max(1, 2 * i) * P::kSlot; };  // the first block's is odd, the others' are even
+        const int col = row * D + 4 * (D == 128 ? lane : lane & 15);
 #pragma unroll 1
-        for (int j = 0; j < 32 && i0 + j * subs < n_parts; j += 8) {
+        for (int i0 = sub; i0 < n_parts; i0 += 32 * subs) {
+          const int i = i0 + lane * subs;
+          const bool in = i < n_parts;
           float4 v[8];
+          auto take = [&](int j) {  // parts j .. j + 7 of the 32
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const int k = i0 + (j + u) * subs;
-            v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (k < n_parts) v[u] = __ldcg(reinterpret_cast<const float4*>(part_at(k) + row * D + 4 * (D == 128 ? lane : lane & 15)));
-          }
+            for (int u = 0; u < 8; ++u) {
+              const int k = i0 + (j + u) * subs;
+              v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (k < n_parts) v[u] = __ldcg(reinterpret_cast<const float4*>(part_at(k) + col));
+            }
+          };
+          const float mine = in ? __ldcg(part_at(i) + HT * D + row) : -CUDART_INF_F;
+          const float sum_mine = in ? __ldcg(part_at(i) + HT * D + HT + row) : 0.f;
+          int j = 0;
+          take(0);
+          float to = mine;
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const float f = __shfl_sync(full, weight, j + u);  // 0 behind the last
-            o.x = fmaf(v[u].x, f, o.x); o.y = fmaf(v[u].y, f, o.y); o.z = fmaf(v[u].z, f, o.z); o.w = fmaf(v[u].w, f, o.w);
+          for (int off = 16; off >= 1; off >>= 1) to = fmaxf(to, __shfl_xor_sync(full, to, off));
+          to = fmaxf(to, top);
+          const float alpha = top == to ? 1.f : exp2_approx(top - to), weight = in ? exp2_approx(mine - to) : 0.f;
+          top = to;
+          float all = sum_mine * weight;
+#pragma unroll
+          for (int off = 16; off >= 1; off >>= 1) all += __shfl_xor_sync(full, all, off);
+          sum = fmaf(sum, alpha, all);
+          o.x *= alpha; o.y *= alpha; o.z *= alpha; o.w *= alpha;
+#pragma unroll 1
+          while (true) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+              const float f = __shfl_sync(full, weight, j + u);  // 0 behind the last
+              o.x = fmaf(v[u].x, f, o.x); o.y = fmaf(v[u].y, f, o.y); o.z = fmaf(v[u].z, f, o.z); o.w = fmaf(v[u].w, f, o.w);
+            }
+            j += 8;
+            if (j == 32 || i0 + j * subs >= n_parts) break;
+            take(j);
           }
         }
+        if (subs == 1) {
+          write_row(it, row, top, sum, o);
+        } else {
+          if (D == 128 || lane < 16) *reinterpret_cast<float4*>(part_of(2 * sub + 1) + col) = o;
+          if (lane == 0) { part_m[2 * sub + 1][row] = top; part_l[2 * sub + 1][row] = sum; }
+        }
       }
-      if (D == 128 || lane < 16) *reinterpret_cast<float4*>(part_of(2 * sub + 1) + row * D + 4 * lane) = o;
-      if (lane == 0) { part_m[2 * sub + 1][row] = top; part_l[2 * sub + 1][row] = sum; }
-    }
-    __syncthreads();
-    const unsigned of = 0xaaaaaaaau & (unsigned)((1ull << (2 * min(subs, n_parts))) - 1);
+      if (subs == 1) continue;
+      __syncthreads();
+      const unsigned of = 0xaaaaaaaau & (unsigned)((1ull << (2 * subs)) - 1);
 #pragma unroll 1
-    for (int row = warp; row < rows; row += NW) {
-      float top, sum;
-      float4 o;
-      together(of, row, top, sum, o);
-      write_row(it, row, top, sum, o);
+      for (int row = warp; row < rows; row += NW) {
+        float top, sum;
+        float4 o;
+        together(of, row, top, sum, o);
+        write_row(it, row, top, sum, o);
+      }
+      __syncthreads();
     }
   }
   // sequences without keys
