@@ -131,7 +131,215 @@ struct Item {
 };
 
 template <int D, int kType, int HT>
-__global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged_attention_kernel(const TokenParams p) {
+struct TokenShared {
+  static constexpr int NW = TokenPlan<D, kType, HT>::kWarps;
+  float part_m[2 * NW][HT], part_l[2 * NW][HT];
+  Item part_item[2 * NW];  // whose (n = 0: no part)
+  int part_first[2 * NW];  // its first chunk
+  int last_arrival[2];
+  int x0, x1, each, more;  // the block's share; how the blocks' shares are cut
+};
+// Parts of the block's warps, two of each: of an item that begins before the warp's stretch (in shared memory of its own), and of one that
+// goes on behind it (in the warp's queue, which is empty by then).
+template <int D, int kType, int HT>
+__device__ __forceinline__ float* part_of(uint8_t* dynamic, int i) {
+  using P = TokenPlan<D, kType, HT>;
+  return reinterpret_cast<float*>(i & 1 ? dynamic + (i >> 1) * 8192 : dynamic + P::kQueue + (i >> 1) * P::kPart * 4);
+}
+
+// What follows the loop over the chunks, a function of its own so that it takes no registers from that loop.
+template <int D, int kType, int HT>
+__device__ __noinline__ void join_parts(const TokenParams& p, uint8_t* dynamic, TokenShared<D, kType, HT>& sh) {
+  using P = TokenPlan<D, kType, HT>;
+  constexpr int NW = P::kWarps;
+  constexpr bool kF32 = kType == kTypeF32, kF16 = kType == kTypeE4m3;
+  constexpr unsigned full = 0xffffffffu;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, x0 = sh.x0, x1 = sh.x1, each = sh.each, more = sh.more;
+  auto& part_m = sh.part_m;
+  auto& part_l = sh.part_l;
+  auto& part_item = sh.part_item;
+  auto& part_first = sh.part_first;
+  auto& last_arrival = sh.last_arrival;
+  auto part_of = [&](int i) { return tsd::part_of<D, kType, HT>(dynamic, i); };
+  auto block_of = [&](int x) {
+    const bool longer = x < more * (each + 1);
+    return (longer ? 0 : more) + (int)((unsigned)(longer ? x : x - more * (each + 1)) / (unsigned)(each + (longer ? 1 : 0)));
+  };
+  // ---- the block's parts: put together where they are of one sequence, then written out, or, where other blocks have the rest, to the workspace
+  // Row `row` of the parts in `of`, by one warp: offset, sum and 4 dimensions per lane.
+  auto together = [&](unsigned of, int row, float& top, float& sum, float4& o) {
+    const bool in = (of >> lane) & 1;
+    const float mine = in ? part_m[lane][row] : -CUDART_INF_F;
+    top = mine;
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(full, top, off));
+    const float weight = in ? exp2_approx(mine - top) : 0.f;
+    sum = in ? part_l[lane][row] * weight : 0.f;
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(full, sum, off);
+    o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    while (of) {  // four at a time
+      float4 v[4];
+      float f[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = of ? __ffs(of) - 1 : 0;
+        f[k] = __shfl_sync(full, weight, i);
+        if (!of) f[k] = 0.f;
+        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (of) v[k] = *reinterpret_cast<const float4*>(part_of(i) + row * D + 4 * (D == 128 ? lane : lane & 15));
+        of &= of - 1;  // 0 stays 0
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        o.x = fmaf(v[k].x, f[k], o.x); o.y = fmaf(v[k].y, f[k], o.y); o.z = fmaf(v[k].z, f[k], o.z); o.w = fmaf(v[k].w, f[k], o.w);
+      }
+    }
+  };
+  auto write_row = [&](const Item& item, int row, float top, float sum, const float4& o) {
+    const float v_scale = kF16 && p.cache.v_scale ? p.cache.v_scale[item.kv] : 1.f, f = kF32 ? v_scale / sum : __fdividef(v_scale, sum);
+    const int head = item.h0 + row;
+    const int64_t to = item.s * p.o_b + (int64_t)head * p.o_h + 4 * lane;
+    if (D == 128 || lane < 16) {
+      if constexpr (kF32) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to) = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+      else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + to) = make_uint2(bf16_pair(o.x * f, o.y * f), bf16_pair(o.z * f, o.w * f));
+    }
+    if (p.lse && lane == 0) p.lse[(int64_t)item.s * p.Hq + head] = (top + log2f(sum)) * kLn2;
+  };
+  __syncthreads();
+  int shared0 = 0, shared1 = 0, n_shared = 0;  // parts with which items of several blocks begin in this one: at most two
+  {
+    const bool there = lane < 2 * NW && part_item[lane].n > 0;
+    const unsigned valid = __ballot_sync(full, there);
+    const int id = there ? part_first[lane] : -1;  // items are told apart by their first chunk
+    const unsigned below = valid & ((1u << lane) - 1u);
+    const int id_before = __shfl_sync(full, id, below ? 31 - __clz(below) : lane);
+    const unsigned starts = __ballot_sync(full, there && (!below || id_before != id));
+    int turn = 0;  // rows are dealt to the warps in turn
+#pragma unroll 1
+    for (unsigned st = starts; st; st &= st - 1) {
+      const int i = __ffs(st) - 1;
+      const unsigned rest = st & (st - 1), of = valid & ~((1u << i) - 1u) & (rest ? (rest & -rest) - 1u : 0xffffffffu);
+      const Item it = part_item[i];
+      const int first = part_first[i], rows = it.rows;
+      const bool whole = first >= x0 && first + it.n <= x1;
+      float* slot = p.parts + (2 * (int)blockIdx.x + (first < x0 ? 0 : 1)) * P::kSlot;
+#pragma unroll 1
+      for (int row = warp >= turn ? warp - turn : warp - turn + NW; row < rows; row += NW) {
+        float top, sum;
+        float4 o;
+        together(of, row, top, sum, o);
+        if (whole) {
+          write_row(it, row, top, sum, o);
+        } else {
+          if (D == 128 || lane < 16) *reinterpret_cast<float4*>(slot + row * D + 4 * lane) = o;
+          if (lane == 0) { slot[HT * D + row] = top; slot[HT * D + HT + row] = sum; }
+        }
+      }
+      turn = (turn + rows) % NW;
+      if (!whole) {
+        if (n_shared == 0) shared0 = i;
+        else shared1 = i;
+        ++n_shared;
+      }
+    }
+  }
+  // An item of several blocks: the last of them to arrive puts its parts together.  The barrier puts the block's writes before
+  // the arrivals, whose release and acquire take them to the block that arrives last.
+  if (n_shared > 0) {
+    __syncthreads();
+    if (warp < n_shared && lane == 0) {
+      const int i0 = warp == 0 ? shared0 : shared1, b_first = block_of(part_first[i0]);
+      const int n_parts = block_of(part_first[i0] + part_item[i0].n - 1) - b_first + 1;
+      unsigned before;
+      asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(p.tickets + b_first) : "memory");
+      const bool last = before + 1 == (unsigned)n_parts;
+      last_arrival[warp] = last;
+      if (last) p.tickets[b_first] = 0;
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int k = 0; k < n_shared; ++k) {
+      if (!last_arrival[k]) continue;
+      const int i0 = k == 0 ? shared0 : shared1;
+      const Item it = part_item[i0];
+      const int first = part_first[i0], rows = it.rows, b_first = block_of(first), n_parts = block_of(first + it.n - 1) - b_first + 1;
+      // A row by one warp; many parts, and warps to spare: by `subs` warps, each with parts sub, sub + subs, ... , and what they come
+      // to meets in the shared memory of their second parts.  32 parts at a time, a lane for the offset and sum of each.
+      const int subs = n_parts <= 32 ? 1 : max(1, (int)((unsigned)NW / (unsigned)rows));
+      const float* const parts = p.parts + 2 * b_first * P::kSlot;
+#pragma unroll 1
+      for (int task = warp; task < rows * subs; task += NW) {
+        const int sub = (int)((unsigned)task / (unsigned)rows), row = task - sub * rows;
+        float top = -CUDART_INF_F, sum = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto part_at = [&](int i) { return parts + max(1, 2 * i) * P::kSlot; };  // the first block's is odd, the others' are even
+        const int col = row * D + 4 * (D == 128 ? lane : lane & 15);
+#pragma unroll 1
+        for (int i0 = sub; i0 < n_parts; i0 += 32 * subs) {
+          const int i = i0 + lane * subs;
+          const bool in = i < n_parts;
+          float4 v[8];
+          auto take = [&](int j) {  // parts j .. j + 7 of the 32
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+              const int k = i0 + (j + u) * subs;
+              v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (k < n_parts) v[u] = __ldcg(reinterpret_cast<const float4*>(part_at(k) + col));
+            }
+          };
+          const float mine = in ? __ldcg(part_at(i) + HT * D + row) : -CUDART_INF_F;
+          const float sum_mine = in ? __ldcg(part_at(i) + HT * D + HT + row) : 0.f;
+          int j = 0;
+          take(0);
+          float to = mine;
+#pragma unroll
+          for (int off = 16; off >= 1; off >>= 1) to = fmaxf(to, __shfl_xor_sync(full, to, off));
+          to = fmaxf(to, top);
+          const float alpha = top == to ? 1.f : exp2_approx(top - to), weight = in ? exp2_approx(mine - to) : 0.f;
+          top = to;
+          float all = sum_mine * weight;
+#pragma unroll
+          for (int off = 16; off >= 1; off >>= 1) all += __shfl_xor_sync(full, all, off);
+          sum = fmaf(sum, alpha, all);
+          o.x *= alpha; o.y *= alpha; o.z *= alpha; o.w *= alpha;
+#pragma unroll 1
+          while (true) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+              const float f = __shfl_sync(full, weight, j + u);  // 0 behind the last
+              o.x = fmaf(v[u].x, f, o.x); o.y = fmaf(v[u].y, f, o.y); o.z = fmaf(v[u].z, f, o.z); o.w = fmaf(v[u].w, f, o.w);
+            }
+            j += 8;
+            if (j == 32 || i0 + j * subs >= n_parts) break;
+            take(j);
+          }
+        }
+        if (subs == 1) {
+          write_row(it, row, top, sum, o);
+        } else {
+          if (D == 128 || lane < 16) *reinterpret_cast<float4*>(part_of(2 * sub + 1) + col) = o;
+          if (lane == 0) { part_m[2 * sub + 1][row] = top; part_l[2 * sub + 1][row] = sum; }
+        }
+      }
+      if (subs == 1) continue;
+      __syncthreads();
+      const unsigned of = 0xaaaaaaaau & (unsigned)((1ull << (2 * subs)) - 1);
+#pragma unroll 1
+      for (int row = warp; row < rows; row += NW) {
+        float top, sum;
+        float4 o;
+        together(of, row, top, sum, o);
+        write_row(it, row, top, sum, o);
+      }
+      __syncthreads();
+    }
+  }
+}
+
+template <int D, int kType, int HT>
+__global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged_attention_kernel(const __grid_constant__ TokenParams p) {
   using P = TokenPlan<D, kType, HT>;
   constexpr int NW = P::kWarps, KC = P::kKeys, NG = P::kGroups, NP = P::kPieces, NT = HT / 8;
   constexpr bool kF32 = kType == kTypeF32, kF16 = kType == kTypeE4m3;  // e4m3 is a subset of f16
@@ -139,14 +347,8 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   constexpr bool kSplitRuns = kType == kTypeBf16 && D == 128;  // where the tiles' second dimensions lie
   constexpr int kAcc = kF32 ? HT : kTiles * NT;        // rows of 4 dimensions (fp32), or tiles of 16 dimensions x 8 heads
   extern __shared__ __align__(16) uint8_t dynamic[];
-  // Parts of the block's warps, two of each: of an item that begins before the warp's stretch (in shared memory of its own), and of one that
-  // goes on behind it (in the warp's queue, which is empty by then).
-  auto part_of = [&](int i) { return reinterpret_cast<float*>(i & 1 ? dynamic + (i >> 1) * 8192 : dynamic + P::kQueue + (i >> 1) * P::kPart * 4); };
-  __shared__ float part_m[2 * NW][HT], part_l[2 * NW][HT];
-  __shared__ Item part_item[2 * NW];                          // whose (n = 0: no part)
-  __shared__ int part_first[2 * NW];                          // its first chunk
+  __shared__ TokenShared<D, kType, HT> shared;
   __shared__ __align__(16) float weights[kF32 ? NW : 1][kF32 ? KC : 1][HT];
-  __shared__ int last_arrival[2];
   static_assert(2 * NW <= 32, "a lane per part");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   constexpr unsigned full = 0xffffffffu;
@@ -170,12 +372,9 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   const int n_blocks = max(1, min((int)gridDim.x, (total + NW - 1) / NW));
   const int each = (int)((unsigned)total / (unsigned)n_blocks), more = total - each * n_blocks;
   auto first_of = [&](int b) { return b * each + min(b, more); };
-  auto block_of = [&](int x) {
-    const bool longer = x < more * (each + 1);
-    return (longer ? 0 : more) + (int)((unsigned)(longer ? x : x - more * (each + 1)) / (unsigned)(each + (longer ? 1 : 0)));
-  };
   const bool idle = (int)blockIdx.x >= n_blocks;
   const int x0 = idle ? total : first_of(blockIdx.x), x1 = idle ? total : first_of(blockIdx.x + 1);
+  if (tid == 0) { shared.x0 = x0; shared.x1 = x1; shared.each = each; shared.more = more; }
   // and its warps an even share of that, [w0, w1) for this one
   const unsigned share = (unsigned)(x1 - x0) / NW, longer = (unsigned)(x1 - x0) % NW;
   const int w0 = x0 + (int)(warp * share + min((unsigned)warp, longer)), w1 = w0 + (int)(share + (warp < (int)longer ? 1 : 0));
@@ -340,19 +539,19 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   };
   // What an item's chunks have come to so far: put aside as part i of the block, or, if they are all of it, written out.
   auto put_aside = [&](const Item& item, int first, int i) {
-    float* o = part_of(i);
+    float* o = part_of<D, kType, HT>(dynamic, i);
     const int rows = item.rows;
-    if (lane == 0) { part_item[i] = item; part_first[i] = first; }
+    if (lane == 0) { shared.part_item[i] = item; shared.part_first[i] = first; }
     if constexpr (kF32) {
 #pragma unroll
       for (int r = 0; r < HT; ++r)
         if (r < rows && (D == 128 || lane < 16)) *reinterpret_cast<float4*>(o + r * D + 4 * lane) = make_float4(acc[r][0], acc[r][1], acc[r][2], acc[r][3]);
-      if (lane < HT) { part_m[i][lane] = m[0]; part_l[i][lane] = l[0]; }
+      if (lane < HT) { shared.part_m[i][lane] = m[0]; shared.part_l[i][lane] = l[0]; }
     } else {
 #pragma unroll
       for (int h = 0; h < 2 * NT; ++h) {
         const int head = 8 * (h >> 1) + 2 * t + (h & 1);
-        if (g == 0) { part_m[i][head] = m[h]; part_l[i][head] = l[h]; }
+        if (g == 0) { shared.part_m[i][head] = m[h]; shared.part_l[i][head] = l[h]; }
         if (head < rows) {
 #pragma unroll
           for (int run = 0; run < 2; ++run)
@@ -403,7 +602,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   };
 
   // ---- the warp's chunks.  The round before the first one only fetches.
-  if (lane < 2) part_item[2 * warp + lane].n = 0;
+  if (lane < 2) shared.part_item[2 * warp + lane].n = 0;
   __syncwarp();
   Item item = next;                                     // at hand, and its chunk;
   int c = 0, left = 0;                                  // how many of the chunk's keys count
@@ -719,177 +918,8 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
     }
   }
 
-  // ---- the block's parts: put together where they are of one sequence, then written out, or, where other blocks have the rest, to the workspace
-  // Row `row` of the parts in `of`, by one warp: offset, sum and 4 dimensions per lane.
-  auto together = [&](unsigned of, int row, float& top, float& sum, float4& o) {
-    const bool in = (of >> lane) & 1;
-    const float mine = in ? part_m[lane][row] : -CUDART_INF_F;
-    top = mine;
-#pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(full, top, off));
-    const float weight = in ? exp2_approx(mine - top) : 0.f;
-    sum = in ? part_l[lane][row] * weight : 0.f;
-#pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(full, sum, off);
-    o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-    while (of) {  // four at a time
-      float4 v[4];
-      float f[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int i = of ? __ffs(of) - 1 : 0;
-        f[k] = __shfl_sync(full, weight, i);
-        if (!of) f[k] = 0.f;
-        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (of) v[k] = *reinterpret_cast<const float4*>(part_of(i) + row * D + 4 * (D == 128 ? lane : lane & 15));
-        of &= of - 1;  // 0 stays 0
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        o.x = fmaf(v[k].x, f[k], o.x); o.y = fmaf(v[k].y, f[k], o.y); o.z = fmaf(v[k].z, f[k], o.z); o.w = fmaf(v[k].w, f[k], o.w);
-      }
-    }
-  };
-  auto write_row = [&](const Item& item, int row, float top, float sum, const float4& o) {
-    const float v_scale = kF16 && a.cache.v_scale ? a.cache.v_scale[item.kv] : 1.f, f = kF32 ? v_scale / sum : __fdividef(v_scale, sum);
-    const int head = item.h0 + row;
-    const int64_t to = item.s * a.o_b + (int64_t)head * a.o_h + 4 * lane;
-    if (D == 128 || lane < 16) {
-      if constexpr (kF32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
-      else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + to) = make_uint2(bf16_pair(o.x * f, o.y * f), bf16_pair(o.z * f, o.w * f));
-    }
-    if (a.lse && lane == 0) a.lse[(int64_t)item.s * a.Hq + head] = (top + log2f(sum)) * kLn2;
-  };
-  __syncthreads();
-  int shared0 = 0, shared1 = 0, n_shared = 0;  // parts with which items of several blocks begin in this one: at most two
-  {
-    const bool there = lane < 2 * NW && part_item[lane].n > 0;
-    const unsigned valid = __ballot_sync(full, there);
-    const int id = there ? part_first[lane] : -1;  // items are told apart by their first chunk
-    const unsigned below = valid & ((1u << lane) - 1u);
-    const int id_before = __shfl_sync(full, id, below ? 31 - __clz(below) : lane);
-    const unsigned starts = __ballot_sync(full, there && (!below || id_before != id));
-    int turn = 0;  // rows are dealt to the warps in turn
-#pragma unroll 1
-    for (unsigned st = starts; st; st &= st - 1) {
-      const int i = __ffs(st) - 1;
-      const unsigned rest = st & (st - 1), of = valid & ~((1u << i) - 1u) & (rest ? (rest & -rest) - 1u : 0xffffffffu);
-      const Item it = part_item[i];
-      const int first = part_first[i], rows = it.rows;
-      const bool whole = first >= x0 && first + it.n <= x1;
-      float* slot = a.parts + (2 * (int)blockIdx.x + (first < x0 ? 0 : 1)) * P::kSlot;
-#pragma unroll 1
-      for (int row = warp >= turn ? warp - turn : warp - turn + NW; row < rows; row += NW) {
-        float top, sum;
-        float4 o;
-        together(of, row, top, sum, o);
-        if (whole) {
-          write_row(it, row, top, sum, o);
-        } else {
-          if (D == 128 || lane < 16) *reinterpret_cast<float4*>(slot + row * D + 4 * lane) = o;
-          if (lane == 0) { slot[HT * D + row] = top; slot[HT * D + HT + row] = sum; }
-        }
-      }
-      turn = (turn + rows) % NW;
-      if (!whole) {
-        if (n_shared == 0) shared0 = i;
-        else shared1 = i;
-        ++n_shared;
-      }
-    }
-  }
-  // An item of several blocks: the last of them to arrive puts its parts together.  The barrier puts the block's writes before
-  // the arrivals, whose release and acquire take them to the block that arrives last.
-  if (n_shared > 0) {
-    __syncthreads();
-    if (warp < n_shared && lane == 0) {
-      const int i0 = warp == 0 ? shared0 : shared1, b_first = block_of(part_first[i0]);
-      const int n_parts = block_of(part_first[i0] + part_item[i0].n - 1) - b_first + 1;
-      unsigned before;
-      asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.tickets + b_first) : "memory");
-      const bool last = before + 1 == (unsigned)n_parts;
-      last_arrival[warp] = last;
-      if (last) a.tickets[b_first] = 0;
-    }
-    __syncthreads();
-#pragma unroll 1
-    for (int k = 0; k < n_shared; ++k) {
-      if (!last_arrival[k]) continue;
-      const int i0 = k == 0 ? shared0 : shared1;
-      const Item it = part_item[i0];
-      const int first = part_first[i0], rows = it.rows, b_first = block_of(first), n_parts = block_of(first + it.n - 1) - b_first + 1;
-      // A row by one warp; many parts, and warps to spare: by `subs` warps, each with parts sub, sub + subs, ... , and what they come
-      // to meets in the shared memory of their second parts.  32 parts at a time, a lane for the offset and sum of each.
-      const int subs = n_parts <= 32 ? 1 : max(1, (int)((unsigned)NW / (unsigned)rows));
-      const float* const parts = a.parts + 2 * b_first * P::kSlot;
-#pragma unroll 1
-      for (int task = warp; task < rows * subs; task += NW) {
-        const int sub = (int)((unsigned)task / (unsigned)rows), row = task - sub * rows;
-        float top = -CUDART_INF_F, sum = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        auto part_at = [&](int i) { return parts + max(1, 2 * i) * P::kSlot; };  // the first block's is odd, the others' are even
-        const int col = row * D + 4 * (D == 128 ? lane : lane & 15);
-#pragma unroll 1
-        for (int i0 = sub; i0 < n_parts; i0 += 32 * subs) {
-          const int i = i0 + lane * subs;
-          const bool in = i < n_parts;
-          float4 v[8];
-          auto take = [&](int j) {  // parts j .. j + 7 of the 32
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-              const int k = i0 + (j + u) * subs;
-              v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-              if (k < n_parts) v[u] = __ldcg(reinterpret_cast<const float4*>(part_at(k) + col));
-            }
-          };
-          const float mine = in ? __ldcg(part_at(i) + HT * D + row) : -CUDART_INF_F;
-          const float sum_mine = in ? __ldcg(part_at(i) + HT * D + HT + row) : 0.f;
-          int j = 0;
-          take(0);
-          float to = mine;
-#pragma unroll
-          for (int off = 16; off >= 1; off >>= 1) to = fmaxf(to, __shfl_xor_sync(full, to, off));
-          to = fmaxf(to, top);
-          const float alpha = top == to ? 1.f : exp2_approx(top - to), weight = in ? exp2_approx(mine - to) : 0.f;
-          top = to;
-          float all = sum_mine * weight;
-#pragma unroll
-          for (int off = 16; off >= 1; off >>= 1) all += __shfl_xor_sync(full, all, off);
-          sum = fmaf(sum, alpha, all);
-          o.x *= alpha; o.y *= alpha; o.z *= alpha; o.w *= alpha;
-#pragma unroll 1
-          while (true) {
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-              const float f = __shfl_sync(full, weight, j + u);  // 0 behind the last
-              o.x = fmaf(v[u].x, f, o.x); o.y = fmaf(v[u].y, f, o.y); o.z = fmaf(v[u].z, f, o.z); o.w = fmaf(v[u].w, f, o.w);
-            }
-            j += 8;
-            if (j == 32 || i0 + j * subs >= n_parts) break;
-            take(j);
-          }
-        }
-        if (subs == 1) {
-          write_row(it, row, top, sum, o);
-        } else {
-          if (D == 128 || lane < 16) *reinterpret_cast<float4*>(part_of(2 * sub + 1) + col) = o;
-          if (lane == 0) { part_m[2 * sub + 1][row] = top; part_l[2 * sub + 1][row] = sum; }
-        }
-      }
-      if (subs == 1) continue;
-      __syncthreads();
-      const unsigned of = 0xaaaaaaaau & (unsigned)((1ull << (2 * subs)) - 1);
-#pragma unroll 1
-      for (int row = warp; row < rows; row += NW) {
-        float top, sum;
-        float4 o;
-        together(of, row, top, sum, o);
-        write_row(it, row, top, sum, o);
-      }
-      __syncthreads();
-    }
-  }
+  join_parts<D, kType, HT>(p, dynamic, shared);
+
   // sequences without keys
 #pragma unroll 1
   for (int s = (int)(blockIdx.x + gridDim.x * warp); s < a.S; s += (int)gridDim.x * NW) {
