@@ -35,7 +35,7 @@ enum { kTypeF32 = TSD_F32, kTypeBf16 = TSD_BF16, kTypeE4m3 = TSD_E4M3 };
 
 template <int D, int kType, int HT>  // HT: heads per tile, 8 or 16
 struct TokenPlan {
-  static constexpr int kWarps = HT == 8 ? 16 : 12;                             // at 128 and 168 registers a thread
+  static constexpr int kWarps = HT == 8 ? 12 : 8;                              // at 168 and 255 registers a thread
   static constexpr int kSize = kType == kTypeF32 ? 4 : kType == kTypeBf16 ? 2 : 1;  // bytes of a cached element
   static constexpr int kRow = D * kSize;                                       // bytes of a row
   static constexpr int kPieces = kRow / 64;                                    // 16-byte pieces per lane and key
