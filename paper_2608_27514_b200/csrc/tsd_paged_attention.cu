@@ -28,6 +28,7 @@
 namespace tsd {
 
 constexpr int kTokenBlocks = kPlanSms;  // at most: what the workspace is sized for
+constexpr int kAlignSlack = 32;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;           // by how much a score may pass the offset, as a power of 2
 
@@ -137,7 +138,8 @@ struct TokenShared {
   Item part_item[2 * NW];  // whose (n = 0: no part)
   int part_first[2 * NW];  // its first chunk
   int last_arrival[2];
-  int x0, x1, each, more;  // the block's share; how the blocks' shares are cut
+  int x0, x1, each, more;     // the block's share; how the blocks' shares are cut
+  int item_blocks, in_item;
 };
 // Parts of the block's warps, two of each: of an item that begins before the warp's stretch (in shared memory of its own), and of one that
 // goes on behind it (in the warp's queue, which is empty by then).
@@ -164,6 +166,10 @@ __device__ __noinline__ void join_parts(const TokenParams& p, uint8_t* dynamic, 
   auto block_of = [&](int x) {
     const bool longer = x < more * (each + 1);
     return (longer ? 0 : more) + (int)((unsigned)(longer ? x : x - more * (each + 1)) / (unsigned)(each + (longer ? 1 : 0)));
+  };
+  auto blocks_of = [&](int first, int n, int& b_first, int& count) {  // that an item's chunks went to
+    b_first = sh.item_blocks ? (int)blockIdx.x - sh.in_item : block_of(first);
+    count = sh.item_blocks ? sh.item_blocks : block_of(first + n - 1) - b_first + 1;
   };
   // ---- the block's parts: put together where they are of one sequence, then written out, or, where other blocks have the rest, to the workspace
   // Row `row` of the parts in `of`, by one warp: offset, sum and 4 dimensions per lane.
@@ -250,8 +256,9 @@ __device__ __noinline__ void join_parts(const TokenParams& p, uint8_t* dynamic, 
   if (n_shared > 0) {
     __syncthreads();
     if (warp < n_shared && lane == 0) {
-      const int i0 = warp == 0 ? shared0 : shared1, b_first = block_of(part_first[i0]);
-      const int n_parts = block_of(part_first[i0] + part_item[i0].n - 1) - b_first + 1;
+      const int i0 = warp == 0 ? shared0 : shared1;
+      int b_first, n_parts;
+      blocks_of(part_first[i0], part_item[i0].n, b_first, n_parts);
       unsigned before;
       asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(p.tickets + b_first) : "memory");
       const bool last = before + 1 == (unsigned)n_parts;
@@ -264,7 +271,9 @@ __device__ __noinline__ void join_parts(const TokenParams& p, uint8_t* dynamic, 
       if (!last_arrival[k]) continue;
       const int i0 = k == 0 ? shared0 : shared1;
       const Item it = part_item[i0];
-      const int first = part_first[i0], rows = it.rows, b_first = block_of(first), n_parts = block_of(first + it.n - 1) - b_first + 1;
+      const int rows = it.rows;
+      int b_first, n_parts;
+      blocks_of(part_first[i0], it.n, b_first, n_parts);
       // A row by one warp; many parts, and warps to spare: by `subs` warps, each with parts sub, sub + subs, ... , and what they come
       // to meets in the shared memory of their second parts.  32 parts at a time, a lane for the offset and sum of each.
       const int subs = n_parts <= 32 ? 1 : max(1, (int)((unsigned)NW / (unsigned)rows));
@@ -365,16 +374,55 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   for (int s = lane; s < a.S; s += 32) {
     total += chunks(s < 32 ? len0 : length(s));
   }
+  total = __reduce_add_sync(full, total) * HI;
+  // as many blocks as have a chunk for each of their warps
+  const int most_blocks = max(1, min((int)gridDim.x, (total + NW - 1) / NW));
+  const int each = (int)((unsigned)total / (unsigned)most_blocks), more = total - each * most_blocks;
+  // Either the blocks take `each` chunks, the first `more` of them one more, wherever that cuts the items.  Or every item is cut for itself, into
+  // pieces of at most `piece` chunks, one per block: then a block has parts of one item only and one arrival to wait for, which is
+  // worth two chunks and a 32nd, no more.  (4 items of 256 chunks: 86 blocks that straddle items 12.5 us, 80 that do not 11.3.)
+  int x0, x1, item_blocks = 0, in_item = 0;  // of the block's item, in the second case: blocks, and which of them this is
+  const int n0 = chunks(len0);
+  int piece = each + (more > 0), pieces = 0;
+  if (a.S <= 32 && total > 0) {
+#pragma unroll 1
+    for (int tries = 0; tries < 8; ++tries) {
+      pieces = (int)((unsigned)(n0 + piece - 1) / (unsigned)piece);
+      const int blocks = __reduce_add_sync(full, pieces) * HI;
+      if (blocks <= most_blocks) {
+        item_blocks = 1;
+        break;
+      }
+      piece = max(piece + 1, (int)((unsigned)(piece * (int64_t)blocks / most_blocks)));
+      if (piece > each + 2 + each / kAlignSlack) break;
+    }
+  }
+  if (item_blocks) {
+    int blocks_upto = pieces * HI, chunks_upto = n0 * HI;
 #pragma unroll
-  for (int off = 16; off >= 1; off >>= 1) total += __shfl_xor_sync(full, total, off);
-  total *= HI;
-  // blocks (as many as have a chunk for each of their warps) take total / n_blocks chunks each, the first `more` of them one more
-  const int n_blocks = max(1, min((int)gridDim.x, (total + NW - 1) / NW));
-  const int each = (int)((unsigned)total / (unsigned)n_blocks), more = total - each * n_blocks;
-  auto first_of = [&](int b) { return b * each + min(b, more); };
-  const bool idle = (int)blockIdx.x >= n_blocks;
-  const int x0 = idle ? total : first_of(blockIdx.x), x1 = idle ? total : first_of(blockIdx.x + 1);
-  if (tid == 0) { shared.x0 = x0; shared.x1 = x1; shared.each = each; shared.more = more; }
+    for (int off = 1; off < 32; off <<= 1) {
+      const int o = __shfl_up_sync(full, blocks_upto, off), c = __shfl_up_sync(full, chunks_upto, off);
+      if (lane >= off) { blocks_upto += o; chunks_upto += c; }
+    }
+    const unsigned hit = __ballot_sync(full, blocks_upto > (int)blockIdx.x);
+    const int l = hit ? __ffs(hit) - 1 : 0;
+    item_blocks = __shfl_sync(full, pieces, l);
+    const int n = __shfl_sync(full, n0, l), b = (int)blockIdx.x - (__shfl_sync(full, blocks_upto, l) - item_blocks * HI);
+    const int hi = hit ? (int)((unsigned)b / (unsigned)item_blocks) : 0;
+    in_item = b - hi * item_blocks;
+    const int first = __shfl_sync(full, chunks_upto, l) - n * HI + hi * n;
+    const int even = hit ? (int)((unsigned)n / (unsigned)item_blocks) : 0, rest = n - even * item_blocks;
+    x0 = hit ? first + in_item * even + min(in_item, rest) : total;
+    x1 = hit ? x0 + even + (in_item < rest ? 1 : 0) : total;
+  } else {
+    const int b = min((int)blockIdx.x, most_blocks);
+    x0 = b * each + min(b, more);
+    x1 = b == most_blocks ? total : x0 + each + (b < more ? 1 : 0);
+  }
+  if (tid == 0) {
+    shared.x0 = x0; shared.x1 = x1; shared.each = each; shared.more = more;
+    shared.item_blocks = item_blocks; shared.in_item = in_item;
+  }
   // and its warps an even share of that, [w0, w1) for this one
   const unsigned share = (unsigned)(x1 - x0) / NW, longer = (unsigned)(x1 - x0) % NW;
   const int w0 = x0 + (int)(warp * share + min((unsigned)warp, longer)), w1 = w0 + (int)(share + (warp < (int)longer ? 1 : 0));
