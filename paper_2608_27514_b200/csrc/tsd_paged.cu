@@ -1,10 +1,12 @@
 // New rows into a paged K/V cache, with the position rotation on the way (paper App. A: the dual cache is refreshed at block
 // boundaries; a paged cache has no counterpart there).
 //
-// A block takes a row, or several where a row has few heads.  A row's angles, position x inverse frequency, are taken once for all heads: reduced in
-// fp64 to an eighth of a turn around the nearest quarter (a position of 10^6 leaves 1e-10 of an angle there; in fp32 it would leave 0.1),
-// then sine and cosine in fp32, left in shared memory.  Every thread moves units of 16 dimensions of a head: the two chunks of 8 that
-// rotate into each other, or 16 neighbours.  The loads of a batch of units are issued before the angles and the page are looked up.
+// A warp takes a row, or, with few rows, some heads of one.  It walks them in units of 16 dimensions per lane (two chunks of 8, half a head
+// apart: those that rotate into each other, and in any case such that an instruction of the warp touches whole 128-byte lines), with the next kAppendAhead units, of the rows to come too, on their way to shared memory
+// (cp.async; a lane reads back what it has fetched, so nothing is waited for but the lane's own fetches).  A lane's units all have the same
+// place in their heads, so their 8 angles, position x inverse frequency, stay in registers for a row: reduced in fp64 to an eighth of a turn
+// around the nearest quarter (a position of 10^6 leaves 1e-10 of an angle there; in fp32 it would leave 0.1), then sine and cosine in
+// fp32, two per lane and handed on through shared memory.
 // Bound by memory: each row is read once and written once, and nothing but the tables comes on top.
 #include <cuda_fp8.h>
 #include <algorithm>
@@ -44,15 +46,14 @@ PagedView paged_view(const tsd_paged_cache& c) {
   return v;
 }
 
-constexpr int kAppendThreads = 256;
-constexpr int kAppendUnits = 3;   // units of a thread in flight: a row of 32 heads each of queries, keys and values is one batch
-constexpr int kAppendBlocks = 4;  // per SM
-constexpr int kAppendRows = 8;    // rows of a block at most
+constexpr int kAppendWarps = 8;    // of a block
+constexpr int kAppendBlocks = 2;   // per SM
+constexpr int kAppendAhead = 5;    // units on their way, of 32 bytes per lane (fp32: half as many, of 64)
 
 struct AppendParams {
   PagedView cache;
   bool cached;
-  int rows, rows_per_block;       // of all sequences
+  int S, units, parts;            // units of a row per lane; parts that a row is cut into
   int n_blocks, n_rows, Hq, Hkv;  // Hq = 0: no queries
   const int32_t *block, *n_new, *first_slot, *positions;
   const float* inv_freq;
@@ -61,18 +62,15 @@ struct AppendParams {
   uint32_t* status;
 };
 
-struct alignas(16) Chunk8F { float4 a, b; };
-// 8 consecutive elements of a row <-> fp32.  Plain loads: a result may go where its input was.
-__device__ __forceinline__ Chunk8F load_chunk(const float* p) {
-  return {reinterpret_cast<const float4*>(p)[0], reinterpret_cast<const float4*>(p)[1]};
+// 8 consecutive elements <-> fp32.  Ordinary stores: a result may go where its input was.
+__device__ __forceinline__ void widen(const uint4* c, float (&x)[8], float) {  // fp32: the second 16 bytes lie one piece of all lanes on
+  const float4 a = *reinterpret_cast<const float4*>(c), b = *reinterpret_cast<const float4*>(c + 32);
+  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+  x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
 }
-__device__ __forceinline__ uint4 load_chunk(const __nv_bfloat16* p) { return *reinterpret_cast<const uint4*>(p); }
-__device__ __forceinline__ void widen(const Chunk8F& c, float (&x)[8]) {
-  x[0] = c.a.x; x[1] = c.a.y; x[2] = c.a.z; x[3] = c.a.w;
-  x[4] = c.b.x; x[5] = c.b.y; x[6] = c.b.z; x[7] = c.b.w;
-}
-__device__ __forceinline__ void widen(const uint4& c, float (&x)[8]) {
-  const uint32_t u[4] = {c.x, c.y, c.z, c.w};
+__device__ __forceinline__ void widen(const uint4* c, float (&x)[8], __nv_bfloat16) {
+  const uint4 v = *c;
+  const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     x[2 * i] = __uint_as_float(u[i] << 16);
@@ -121,93 +119,145 @@ __device__ __forceinline__ float2 cos_sin(int position, float inv_freq) {
   return make_float2(turn == 1 || turn == 2 ? -cx : cx, turn >= 2 ? -sx : sx);
 }
 
-// kNext: neighbouring dimensions (2j, 2j + 1) form the pairs.  kOne: one row per block; every thread looks up by itself whose it is, without a barrier.
-template <typename T, typename C, int D, bool kNext, bool kOne>
-__global__ void __launch_bounds__(kAppendThreads, kAppendBlocks)
+template <typename T, typename C, int D, bool kNext>  // kNext: neighbouring dimensions (2j, 2j + 1) form the pairs
+__global__ void __launch_bounds__(kAppendWarps * 32, kAppendBlocks)
 append_kernel(const T* k, const T* v, const T* q, T* k_out, T* q_out, AppendParams p) {
-  struct Row {
-    int s, from, slot;  // sequence, row of k, v and q (-1: does not count, -2: its block does not exist), slot in the cache
-    bool in_cache;      // it is one
-  };
-  constexpr int kRows = kOne ? 1 : kAppendRows;
-  __shared__ float2 turns[kRows][D / 2];
-  __shared__ Row rows[kRows];
-  __shared__ int64_t row_at[kRows];  // where the row's page has it, in elements; -1: nowhere
+  constexpr int kPer = D / 16, kHeads = 32 / kPer;               // units per head; heads per unit of a warp
+  constexpr int kPieces = 2 * (int)sizeof(T) / 2;                // 16-byte pieces of a unit: 2, fp32 4
+  constexpr int kAhead = kAppendAhead / (int)(sizeof(T) / 2);
+  __shared__ uint4 queue[kAppendWarps][kAhead][kPieces][32];
+  __shared__ float2 turns[kAppendWarps][D / 2];
+  constexpr unsigned full = 0xffffffffu;
   grid_wait(k, v, q, k_out, q_out);
   settle(p.block, p.n_new, p.first_slot, p.positions, p.inv_freq, p.cache.table, p.cache.k_scale, p.cache.v_scale);
-  const int tid = threadIdx.x, first = (int)blockIdx.x * (kOne ? 1 : p.rows_per_block), count = kOne ? 1 : min(p.rows_per_block, p.rows - first);
-  auto look_up = [&](int f) {
-    const int s = (int)((unsigned)f / (unsigned)p.n_rows), i = f - s * p.n_rows;
-    const int n_new = p.n_new ? p.n_new[s] : p.n_rows, block = p.block ? p.block[s] : 0;
-    const int64_t slot = (int64_t)(p.first_slot ? p.first_slot[s] : 0) + i;
-    const bool there = block >= 0 && block < p.n_blocks;
-    return Row{s, i >= n_new ? -1 : there ? block * p.n_rows + i : -2, (int)slot, slot >= 0 && slot < p.cache.cap};
-  };
-  Row only;
-  if (kOne) {
-    only = look_up(first);
-    if (only.from == -1) return;
-  } else {
-    if (tid < count) rows[tid] = look_up(first + tid);
-    __syncthreads();
-  }
-  auto row_of = [&](int r) -> const Row& { return kOne ? only : rows[r]; };
-
-  // Units of 16 dimensions: heads of q, then of k, then of v, row by row; D / 16 per head.  A thread's units have the same place in their heads.
-  constexpr int kPer = D / 16, kStep = kAppendThreads / kPer;
-  static_assert(kAppendThreads % kPer == 0, "a thread's place in a head stays the same");
-  const int place = tid % kPer, half = p.rot / 2;
-  const bool turning = place * 16 < p.rot;
-  // the unit's two chunks of 8: dimensions [d0, d0 + 8) and [d1, d1 + 8)
-  const int d0_rot = kNext || !turning ? place * 16 : place * 8, d1_rot = kNext || !turning ? place * 16 + 8 : half + place * 8;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, place = lane % kPer, half = p.rot / 2;
+  // A unit's two chunks of 8: dimensions [place * 8, + 8) and [D / 2 + place * 8, + 8).  Halves of rot < D dimensions that rotate into each other
+  // are closer: the first rot / 16 places take these, the others 16 neighbours behind them.
+  const bool closer = !kNext && p.rot > 0 && p.rot < D, turning = kNext ? place * 8 < p.rot : place * 16 < p.rot;
+  const int d0_rot = closer && !turning ? place * 16 : place * 8, d1_rot = !closer ? D / 2 + place * 8 : turning ? half + place * 8 : place * 16 + 8;
   const int heads = p.Hq + p.Hkv + (p.cached ? p.Hkv : 0);
-  int row = 0, head = tid / kPer;  // of the thread's next unit
-  bool waited = false;
-  do {
-    decltype(load_chunk(k)) raw[kAppendUnits][2];
-    int row0 = row, head0 = head;
+
+  // Rows that count, one behind the other (up to 32 sequences; more: all rows, and those that do not count are passed over)
+  const bool counted = p.n_new && p.S <= 32;
+  int upto = 0, n_rows = p.S * p.n_rows;
+  if (counted) {
+    const int mine = lane < p.S ? min(max(p.n_new[lane], 0), p.n_rows) : 0;
+    upto = mine;
 #pragma unroll
-    for (int u = 0; u < kAppendUnits; ++u, head += kStep) {
-      while (head >= heads && row < count) { head -= heads; ++row; }
-      if (row >= count || row_of(row).from < 0) continue;
-      const int64_t s = row_of(row).s, from = row_of(row).from;
-      const T* src = head < p.Hq ? q + s * p.q_b + from * p.q_r + head * p.q_h
-                                 : (head < p.Hq + p.Hkv ? k + (head - p.Hq) * p.kv_h : v + (head - p.Hq - p.Hkv) * p.kv_h) + s * p.kv_b + from * p.kv_r;
-      const bool is_v = head >= p.Hq + p.Hkv;  // values do not turn
-      raw[u][0] = load_chunk(src + (is_v ? place * 16 : d0_rot));
-      raw[u][1] = load_chunk(src + (is_v ? place * 16 + 8 : d1_rot));
+    for (int off = 1; off < 32; off <<= 1) {
+      const int o = __shfl_up_sync(full, upto, off);
+      if (lane >= off) upto += o;
     }
-    if (!waited) {
-      for (int e = tid; e < count * half; e += kAppendThreads) {
-        const int r = kOne ? 0 : (int)((unsigned)e / (unsigned)half), j = e - r * half, f = first + r;
-        if (row_of(r).from >= 0) turns[r][j] = cos_sin(p.positions ? p.positions[f] : row_of(r).slot, p.inv_freq[j]);
+    n_rows = __shfl_sync(full, upto, 31);
+  }
+  struct Row {
+    int s, i;
+    int64_t from;  // row of k, v and q; -1: its block does not exist
+  };
+  auto row_at = [&](int r) {
+    Row row;
+    if (counted) {
+      row.s = __ffs(__ballot_sync(full, upto > r)) - 1;
+      row.i = r - (row.s > 0 ? __shfl_sync(full, upto, row.s - 1) : 0);
+    } else {
+      row.s = (int)((unsigned)r / (unsigned)p.n_rows);
+      row.i = r - row.s * p.n_rows;
+    }
+    const int block = p.block ? p.block[row.s] : 0;
+    row.from = block >= 0 && block < p.n_blocks ? (int64_t)block * p.n_rows + row.i : -1;
+    return row;
+  };
+  // A task is a part of a row: units [first, last).  The warps take the tasks in turn.
+  const int n_tasks = n_rows * p.parts, stride = (int)gridDim.x * kAppendWarps;  // fewer than 2^31: checked on the host
+  struct Task {
+    int t, unit, last;
+    Row row;
+  };
+  auto next_task = [&](int t) {  // the task from t on, in strides, whose row counts; t >= n_tasks: none
+    Task k;
+    for (;; t += stride) {
+      k.t = t;
+      k.unit = k.last = 0;
+      if (t >= n_tasks) return k;
+      const int r = p.parts == 1 ? t : (int)((unsigned)t / (unsigned)p.parts), part = t - r * p.parts;
+      k.row = row_at(r);
+      if (!counted && p.n_new && k.row.i >= p.n_new[k.row.s]) continue;
+      if (k.row.from < 0) {
+        if (lane == 0 && p.status) atomicOr(p.status, TSD_STATUS_BAD_INDEX);
+        continue;
       }
-      if (tid < count) {
-        int64_t at = -1;
-        const Row& mine = row_of(tid);
-        bool missing = mine.from == -2;
-        if (p.cached && mine.from >= 0) {
-          const int page = mine.in_cache ? page_of(p.cache, mine.s, mine.slot) : -1;
-          if (page >= 0) at = (int64_t)page * p.cache.ps_p + (mine.slot & ((1 << p.cache.shift) - 1)) * p.cache.ps_r;
-          else missing = true;
+      k.unit = p.parts == 1 ? 0 : (int)((unsigned)(part * p.units) / (unsigned)p.parts);
+      k.last = p.parts == 1 ? p.units : (int)((unsigned)((part + 1) * p.units) / (unsigned)p.parts);
+      return k;
+    }
+  };
+
+  // what is fetched, kAhead units before it is needed
+  Task ahead = next_task((int)blockIdx.x * kAppendWarps + warp);
+  Task task = ahead;
+  int slot_in = 0, slot_out = 0;
+  const uint32_t queue_at = (uint32_t)__cvta_generic_to_shared(&queue[warp][0][0][lane]);
+  auto fetch = [&] {
+    if (ahead.t < n_tasks) {
+      const int head = ahead.unit * kHeads + lane / kPer;
+      if (head < heads) {
+        const bool is_q = head < p.Hq, is_v = head >= p.Hq + p.Hkv;
+        const T* src = is_q ? q + ahead.row.s * p.q_b + ahead.row.from * p.q_r + head * p.q_h
+                            : (is_v ? v + (head - p.Hq - p.Hkv) * p.kv_h : k + (head - p.Hq) * p.kv_h) + ahead.row.s * p.kv_b + ahead.row.from * p.kv_r;
+        const uint32_t to = queue_at + slot_in * (kPieces * 512);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          const int chunk = i / (kPieces / 2), in = i % (kPieces / 2) * (16 / (int)sizeof(T));
+          const T* from = src + (chunk == 0 ? (is_v ? place * 8 : d0_rot) : (is_v ? D / 2 + place * 8 : d1_rot)) + in;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * 512), "l"(from) : "memory");
         }
-        if (missing && p.status) atomicOr(p.status, TSD_STATUS_BAD_INDEX);
-        row_at[tid] = at;
       }
-      __syncthreads();
-      waited = true;
+      if (++ahead.unit == ahead.last) ahead = next_task(ahead.t + stride);
+      slot_in = slot_in + 1 == kAhead ? 0 : slot_in + 1;
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll 1
+  for (int i = 0; i < kAhead; ++i) fetch();
+
+#pragma unroll 1
+  for (; task.t < n_tasks; task = next_task(task.t + stride)) {
+    // where the row goes, and its angles
+    const int s = task.row.s;
+    const int64_t slot = (int64_t)(p.first_slot ? p.first_slot[s] : 0) + task.row.i, from = task.row.from;
+    int64_t at = -1;
+    if (p.cached) {
+      const int page = slot >= 0 && slot < p.cache.cap ? page_of(p.cache, s, (int)slot) : -1;
+      if (page >= 0) at = (int64_t)page * p.cache.ps_p + (slot & ((1 << p.cache.shift) - 1)) * p.cache.ps_r;
+      else if (lane == 0 && p.status) atomicOr(p.status, TSD_STATUS_BAD_INDEX);
+    }
+    float2 turn[8];
+    if (half > 0) {
+      const int position = p.positions ? p.positions[s * (int64_t)p.n_rows + task.row.i] : (int)slot;
+      __syncwarp();
+#pragma unroll 1
+      for (int j = lane; j < half; j += 32) turns[warp][j] = cos_sin(position, p.inv_freq[j]);
+      __syncwarp();
 #pragma unroll
-    for (int u = 0; u < kAppendUnits; ++u, head0 += kStep) {
-      while (head0 >= heads && row0 < count) { head0 -= heads; ++row0; }
-      if (row0 >= count || row_of(row0).from < 0) continue;
+      for (int j = 0; j < 8; ++j) {  // neighbours: of the first chunk's pairs, then of the second one's
+        const int pair = kNext ? (j < 4 ? 0 : D / 4 - 4) + place * 4 + j : place * 8 + j;
+        turn[j] = pair < half ? turns[warp][pair] : make_float2(1.f, 0.f);
+      }
+    }
+#pragma unroll 1
+    for (int unit = task.unit; unit < task.last; ++unit) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+      __syncwarp();
+      const int head = unit * kHeads + lane / kPer;
       float x[8], y[8];
-      widen(raw[u][0], x);
-      widen(raw[u][1], y);
-      const bool is_v = head0 >= p.Hq + p.Hkv;
-      const int d0 = is_v ? place * 16 : d0_rot, d1 = is_v ? place * 16 + 8 : d1_rot;
+      widen(&queue[warp][slot_out][0][lane], x, T());
+      widen(&queue[warp][slot_out][kPieces / 2][lane], y, T());
+      slot_out = slot_out + 1 == kAhead ? 0 : slot_out + 1;
+      fetch();  // into the place of a unit that has been read
+      if (head >= heads) continue;
+      const bool is_q = head < p.Hq, is_v = head >= p.Hq + p.Hkv;  // values do not turn
+      const int d0 = is_v ? place * 8 : d0_rot, d1 = is_v ? D / 2 + place * 8 : d1_rot;
       if (turning && !is_v) {
-        const float2* turn = turns[row0] + place * 8;
         if (kNext) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -228,37 +278,34 @@ append_kernel(const T* k, const T* v, const T* q, T* k_out, T* q_out, AppendPara
           }
         }
       }
-      const int64_t s = row_of(row0).s, from = row_of(row0).from;
-      if (head0 < p.Hq) {
-        T* dst = q_out + s * p.qo_b + from * p.qo_r + head0 * p.qo_h;
+      if (is_q) {
+        T* dst = q_out + s * p.qo_b + from * p.qo_r + head * p.qo_h;
         store_chunk(dst + d0, x);
         store_chunk(dst + d1, y);
         continue;
       }
-      const int g = head0 - p.Hq - (is_v ? p.Hkv : 0);
+      const int g = head - p.Hq - (is_v ? p.Hkv : 0);
       if (!is_v && k_out) {
         T* dst = k_out + s * p.ko_b + from * p.ko_r + g * p.ko_h;
         store_chunk(dst + d0, x);
         store_chunk(dst + d1, y);
       }
-      const int64_t at = row_at[row0];
       if (at >= 0) {
         const float* scales = is_v ? p.cache.v_scale : p.cache.k_scale;
-        const float unit = sizeof(C) == 1 && scales ? 1.f / scales[g] : 1.f;
+        const float unit_scale = sizeof(C) == 1 && scales ? 1.f / scales[g] : 1.f;
         C* dst = const_cast<C*>(static_cast<const C*>(is_v ? p.cache.v : p.cache.k)) + at + g * p.cache.ps_h;
-        store_cached(dst + d0, x, unit);
-        store_cached(dst + d1, y, unit);
+        store_cached(dst + d0, x, unit_scale);
+        store_cached(dst + d1, y, unit_scale);
       }
     }
-  } while (row < count);
+  }
 }
 
 template <typename T, typename C, int D>
 static cudaError_t launch_append(const tsd_append_args& a, const AppendParams& p, cudaStream_t stream) {
-  const bool one = p.rows_per_block == 1;
-  const auto kernel = a.interleaved ? (one ? append_kernel<T, C, D, true, true> : append_kernel<T, C, D, true, false>)
-                                    : (one ? append_kernel<T, C, D, false, true> : append_kernel<T, C, D, false, false>);
-  return launch(kernel, dim3((unsigned)((p.rows + p.rows_per_block - 1) / p.rows_per_block)), dim3(kAppendThreads), 0, stream,
+  const int64_t tasks = (int64_t)a.batch * a.n_rows * p.parts;
+  const int64_t grid = std::min<int64_t>(kAppendBlocks * kPlanSms, (tasks + kAppendWarps - 1) / kAppendWarps);
+  return launch(a.interleaved ? append_kernel<T, C, D, true> : append_kernel<T, C, D, false>, dim3((unsigned)grid), dim3(kAppendWarps * 32), 0, stream,
                 static_cast<const T*>(a.k), static_cast<const T*>(a.v), static_cast<const T*>(a.q), static_cast<T*>(a.k_out),
                 static_cast<T*>(a.q_out), p);
 }
@@ -315,14 +362,15 @@ extern "C" int tsd_append_paged_kv(const tsd_append_args* args, tsd_stream_t str
   p.cached = a.cache != nullptr;
   if (p.cached) p.cache = tsd::paged_view(*a.cache);
   p.n_blocks = a.n_blocks; p.n_rows = a.n_rows;
-  p.rows = a.batch * a.n_rows;
+  p.S = a.batch;
   p.Hq = a.q ? a.n_q_heads : 0; p.Hkv = a.n_kv_heads;
   p.block = a.block; p.n_new = a.n_new; p.first_slot = a.first_slot; p.positions = a.positions;
   p.inv_freq = a.inv_freq;
   p.rot = a.rotary_dim;
-  // as many rows to a block as make one batch of units, if that leaves every SM its four blocks
-  const int units = (p.Hq + p.Hkv * (p.cached ? 2 : 1)) * (a.head_dim / 16);
-  p.rows_per_block = std::max(1, std::min({tsd::kAppendRows, tsd::kAppendThreads * tsd::kAppendUnits / units, p.rows / (tsd::kAppendBlocks * tsd::kPlanSms)}));
+  // a row is cut where there are fewer rows than warps
+  const int per = 32 / (a.head_dim / 16);
+  p.units = (p.Hq + p.Hkv * (p.cached ? 2 : 1) + per - 1) / per;
+  p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(p.units, tsd::kAppendBlocks * tsd::kPlanSms * tsd::kAppendWarps / ((int64_t)a.batch * a.n_rows)));
   p.kv_b = a.kv_stride[0]; p.kv_r = a.kv_stride[1]; p.kv_h = a.kv_stride[2];
   p.q_b = a.q_stride[0]; p.q_r = a.q_stride[1]; p.q_h = a.q_stride[2];
   p.ko_b = a.k_out_stride[0]; p.ko_r = a.k_out_stride[1]; p.ko_h = a.k_out_stride[2];
