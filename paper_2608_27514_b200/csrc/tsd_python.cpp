@@ -432,14 +432,16 @@ T* vec(PyObject* t, PyObject* dtype, int64_t count, const Here& here, const char
 }
 struct Rows {  // [batch, rows, heads, dim], dim contiguous
   int64_t n[4], st[4];
+  PyObject* dtype;  // borrowed: torch's types live as long as torch
   Rows(PyObject* t, const Here& here) {
     here(t);
+    Ref d(PyObject_GetAttr(t, n_dtype));
+    dtype = d.p;
     want(shape(t, n) == 4, "[sequences, rows, heads, head_dim] is wanted");
     want(strides(t, st) == 4 && (n[3] == 1 || st[3] == 1), "head_dim must be contiguous");
   }
-  void as(PyObject* t, const Rows& o, bool heads_too, PyObject* u) const {  // `t`, these rows, has the type and the sizes of `u`
-    Ref a(PyObject_GetAttr(t, n_dtype)), b(PyObject_GetAttr(u, n_dtype));
-    want(a.p == b.p, "types differ");
+  void as(const Rows& o, bool heads_too) const {  // has the type and the sizes of others
+    want(dtype == o.dtype, "types differ");
     want(n[0] == o.n[0] && n[1] == o.n[1] && (!heads_too || n[2] == o.n[2]) && n[3] == o.n[3], "shapes differ");
   }
   void along(const Rows& o) const {  // one set of strides serves both (where a dimension has one entry, any stride does)
@@ -459,7 +461,7 @@ PyObject* append_paged(Args a) {
   const Here here;
   tsd_append_args t = {};
   const Rows k(a[1], here);
-  t.dtype = dtype_code(a[1]);
+  t.dtype = k.dtype == dtype_bf16 ? (int32_t)TSD_BF16 : dtype_code(a[1]);
   k.to(t.kv_stride);
   t.batch = small(k.n[0]);
   t.n_rows = a[12] == Py_None ? small(k.n[1]) : to_i32(a[12]);
@@ -471,15 +473,15 @@ PyObject* append_paged(Args a) {
   t.k = ptr(a[1]);
   if (a[2] != Py_None) {
     const Rows v(a[2], here);
-    v.as(a[2], k, true, a[1]);
+    v.as(k, true);
     v.along(k);
     t.v = ptr(a[2]);
   }
   if (a[8] != Py_None) {
     want(a[9] != Py_None, "q wants a q_out");
     const Rows q(a[8], here), o(a[9], here);
-    q.as(a[8], k, false, a[1]);
-    o.as(a[9], q, true, a[8]);
+    q.as(k, false);
+    o.as(q, true);
     t.n_q_heads = small(q.n[2]);
     q.to(t.q_stride);
     o.to(t.q_out_stride);
@@ -490,7 +492,7 @@ PyObject* append_paged(Args a) {
   }
   if (a[10] != Py_None) {
     const Rows o(a[10], here);
-    o.as(a[10], k, true, a[1]);
+    o.as(k, true);
     o.to(t.k_out_stride);
     t.k_out = ptr(a[10]);
   }
@@ -541,11 +543,11 @@ PyObject* verify_attention_paged(Args a) {
   const Rows q(a[2], here), k(a[4], here), v(a[5], here), o(a[6], here);
   want(q.n[0] == l->batch && q.n[1] == (int64_t)l->n_branches * l->rows_per_branch && q.n[2] == l->n_q_heads && q.n[3] == l->head_dim,
        "q is [batch, branches * rows, n_q_heads, head_dim] of the layout");
-  k.as(a[4], q, false, a[2]);
+  k.as(q, false);
   want(k.n[2] == l->n_kv_heads && dtype_code(a[2]) == l->dtype, "draft rows have the layout's heads and type");
-  v.as(a[5], k, true, a[4]);
+  v.as(k, true);
   v.along(k);
-  o.as(a[6], q, true, a[2]);
+  o.as(q, true);
   here(a[1]);
   here(a[9]);
   here(a[11]);
