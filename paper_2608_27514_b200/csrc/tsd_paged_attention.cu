@@ -355,7 +355,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   constexpr int kTiles = D / 16;                       // of 16 dimensions
   constexpr bool kSplitRuns = kType == kTypeBf16 && D == 128;  // where the tiles' second dimensions lie
   constexpr int kAcc = kF32 ? HT : kTiles * NT;        // rows of 4 dimensions (fp32), or tiles of 16 dimensions x 8 heads
-  extern __shared__ __align__(16) uint8_t dynamic[];
+  extern __shared__ __align__(128) uint8_t dynamic[];  // the queues on whole lines: 16 or 64 bytes beside them cost 4-9 %
   __shared__ TokenShared<D, kType, HT> shared;
   __shared__ __align__(16) float weights[kF32 ? NW : 1][kF32 ? KC : 1][HT];
   static_assert(2 * NW <= 32, "a lane per part");
