@@ -688,7 +688,8 @@ int tsd_append_paged_kv(const tsd_append_args* args, tsd_stream_t stream);
  *   workspace  device, 16-byte aligned, tsd_paged_attention_workspace_bytes() bytes: parts of sequences that
  *              several thread blocks share, and ticket words.  Zero it once before its first use; a completed call leaves every ticket
  *              word at 0.  Two calls that may overlap on the GPU need a workspace each; other shapes may share one.
- * The sequences' lengths together are cut evenly over the GPU, whatever the single ones are.
+ * out must not overlap q.  The sequences' lengths together are cut over the GPU, whatever the single ones are; were all of them full, they have to be
+ * fewer than 2^30 pieces of 4 KB of keys (else TSD_ERR_UNSUPPORTED).
  * ------------------------------------------------------------------------- */
 size_t tsd_paged_attention_workspace_bytes(const tsd_paged_cache* cache, int32_t n_q_heads);
 int tsd_paged_attention(const tsd_paged_cache* cache, int32_t n_q_heads, int32_t dtype, const void* q,

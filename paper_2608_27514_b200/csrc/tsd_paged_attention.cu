@@ -140,6 +140,7 @@ struct TokenShared {
   int last_arrival[2];
   int x0, x1, each, more;     // the block's share; how the blocks' shares are cut
   int item_blocks, in_item;
+  int warp_chunks[NW], run_first[NW * 32];  // of more than 32 sequences: chunks of a warp's runs, in front of a thread's run
 };
 // Parts of the block's warps, two of each: of an item that begins before the warp's stretch (in shared memory of its own), and of one that
 // goes on behind it (in the warp's queue, which is empty by then).
@@ -147,6 +148,39 @@ template <int D, int kType, int HT>
 __device__ __forceinline__ float* part_of(uint8_t* dynamic, int i) {
   using P = TokenPlan<D, kType, HT>;
   return reinterpret_cast<float*>(i & 1 ? dynamic + (i >> 1) * 8192 : dynamic + P::kQueue + (i >> 1) * P::kPart * 4);
+}
+
+__device__ __forceinline__ int length_of(const TokenParams& p, int s) { return p.lens ? min(max(p.lens[s], 0), p.cache.cap) : p.cache.cap; }
+
+// The item behind another one.
+template <int KC, int HT>
+__device__ __forceinline__ Item item_after(const TokenParams& p, Item i) {
+  constexpr unsigned full = 0xffffffffu;
+  i.h0 += i.rows;
+  const int in_group = i.h0 - i.kv * p.group;  // heads of the kv head that are behind us
+  if (in_group == p.group && ++i.kv == p.Hkv) {
+    const int lane = threadIdx.x & 31;
+    i.kv = i.h0 = 0;
+    // the next sequence that has keys, 32 at a time; behind the last one: never fetched
+    int s0 = i.s + 1;
+    i.s = p.S;
+    i.len = 0;
+    i.n = 0x7fffffff;
+#pragma unroll 1
+    for (; s0 < p.S; s0 += 32) {
+      const int len = s0 + lane < p.S ? length_of(p, s0 + lane) : 0;
+      const unsigned some = __ballot_sync(full, len > 0);
+      if (some) {
+        const int l = __ffs(some) - 1;
+        i.s = s0 + l;
+        i.len = __shfl_sync(full, len, l);
+        i.n = (int)(((unsigned)i.len + KC - 1) / KC);
+        break;
+      }
+    }
+  }
+  i.rows = min(HT, (i.kv + 1) * p.group - i.h0);
+  return i;
 }
 
 // What follows the loop over the chunks, a function of its own so that it takes no registers from that loop.
@@ -364,17 +398,34 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   TokenParams a = p;
   grid_wait(a.cache.k, a.cache.v, a.cache.table, a.q, a.lens, a.cache.k_scale, a.cache.v_scale);
   const int HI = a.Hkv * a.tiles;  // items of a sequence
-  auto length = [&](int s) { return a.lens ? min(max(a.lens[s], 0), a.cache.cap) : a.cache.cap; };
+  auto length = [&](int s) { return length_of(a, s); };
   auto chunks = [&](int len) { return (int)(((unsigned)len + KC - 1) / KC); };
 
   // ---- this block's share [x0, x1) of all chunks (fewer than 2^30: checked on the host)
-  int total = 0;
+  // Up to 32 sequences: a lane each, every warp for itself.  More: a thread for a run of them, whose chunks are added up over the block.
+  int total;
   const int len0 = lane < a.S ? length(lane) : 0;  // of the first 32 sequences
-#pragma unroll 1
-  for (int s = lane; s < a.S; s += 32) {
-    total += chunks(s < 32 ? len0 : length(s));
+  const int run = a.S <= 32 ? 0 : (int)((unsigned)(a.S + NW * 32 - 1) / (NW * 32));
+  if (run == 0) {
+    total = __reduce_add_sync(full, chunks(len0));
+  } else {
+    int mine = 0;
+#pragma unroll 4
+    for (int k = 0; k < run; ++k) mine += tid * run + k < a.S ? chunks(length(tid * run + k)) : 0;
+    int upto = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int o = __shfl_up_sync(full, upto, off);
+      if (lane >= off) upto += o;
+    }
+    if (lane == 31) shared.warp_chunks[warp] = upto;
+    __syncthreads();
+    const int of_warp = lane < NW ? shared.warp_chunks[lane] : 0;
+    total = __reduce_add_sync(full, of_warp);
+    shared.run_first[tid] = upto - mine + __reduce_add_sync(full, lane < warp ? of_warp : 0);
+    __syncthreads();
   }
-  total = __reduce_add_sync(full, total) * HI;
+  total *= HI;
   // as many blocks as have a chunk for each of their warps
   const int most_blocks = max(1, min((int)gridDim.x, (total + NW - 1) / NW));
   const int each = (int)((unsigned)total / (unsigned)most_blocks), more = total - each * most_blocks;
@@ -434,25 +485,36 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
     int before = 0;
     next.s = 0;
     next.len = 0;
-#pragma unroll 1
-    for (int s0 = 0; s0 < a.S; s0 += 32) {
-      const int len = s0 == 0 ? len0 : s0 + lane < a.S ? length(s0 + lane) : 0;
-      const int mine = chunks(len) * HI;
+    if (run == 0) {
+      const int mine = chunks(len0) * HI;
       int upto = mine;
 #pragma unroll
       for (int off = 1; off < 32; off <<= 1) {
         const int o = __shfl_up_sync(full, upto, off);
         if (lane >= off) upto += o;
       }
-      const unsigned hit = __ballot_sync(full, before + upto > w0);
+      const unsigned hit = __ballot_sync(full, upto > w0);
       if (hit) {
-        const int l = __ffs(hit) - 1;
-        next.s = s0 + l;
-        next.len = __shfl_sync(full, len, l);
-        before += __shfl_sync(full, upto - mine, l);
-        break;
+        next.s = __ffs(hit) - 1;
+        next.len = __shfl_sync(full, len0, next.s);
+        before = __shfl_sync(full, upto - mine, next.s);
       }
-      before += __shfl_sync(full, upto, 31);
+    } else if (w0 < total) {
+      int lo = 0, hi = NW * 32 - 1;  // the last run that begins at or before w0: no run of empty sequences begins behind it
+#pragma unroll 1
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (shared.run_first[mid] * HI <= w0) lo = mid;
+        else hi = mid - 1;
+      }
+      before = shared.run_first[lo] * HI;
+      next.s = lo * run;
+      next.len = length(next.s);
+#pragma unroll 1
+      while (before + chunks(next.len) * HI <= w0) {  // ends: the chunk exists
+        before += chunks(next.len) * HI;
+        next.len = length(++next.s);
+      }
     }
     next.n = max(chunks(next.len), 1);
     const int hi = (int)((unsigned)(w0 - before) / (unsigned)next.n);
@@ -462,25 +524,6 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
     next.h0 = next.kv * a.group + tile * HT;
     next.rows = min(HT, a.group - tile * HT);
   }
-  auto item_after = [&](Item i) {
-    i.h0 += i.rows;
-    const int in_group = i.h0 - i.kv * a.group;  // heads of the kv head that are behind us
-    if (in_group == a.group && ++i.kv == a.Hkv) {
-      i.kv = i.h0 = 0;
-      do {
-        if (++i.s >= a.S) {  // behind the last chunk: never fetched
-          i.len = 0;
-          i.n = 0x7fffffff;
-          break;
-        }
-        i.len = length(i.s);
-        i.n = chunks(i.len);
-      } while (i.n == 0);
-    }
-    i.rows = min(HT, (i.kv + 1) * a.group - i.h0);
-    return i;
-  };
-
   const int row_mask = (1 << a.cache.shift) - 1;
   const int64_t row_bytes = a.cache.ps_r * P::kSize, page_bytes = a.cache.ps_p * P::kSize, head_bytes = a.cache.ps_h * P::kSize;
   // lane i < NG: the table's entry for the chunk's keys [8 i, 8 i + 8)
@@ -960,9 +1003,11 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
     fresh = ends;
     if (ends && more_chunks) {
       item = next;
-      next = item_after(next);
-      next_c = 0;
-      next_entry = entry_of(next, 0);
+      if (x + 1 + item.n - c < w1) {  // the warp has chunks of another one behind it
+        next = item_after<KC, HT>(p, next);
+        next_c = 0;
+        next_entry = entry_of(next, 0);
+      }
     }
   }
 

@@ -321,6 +321,25 @@ def test_many_sequences_and_repeats():
         assert torch.equal(out, again) and torch.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("S,every,longest", [(31, 2, 40), (32, 32, 900), (33, 1, 20), (64, 64, 700), (385, 3, 60), (2000, 300, 400), (5000, 7, 12)])
+def test_few_sequences_among_many_slots(S, every, longest):
+    # a batch with slots to spare: most sequences are empty, at both ends and in long runs between the others
+    rng = np.random.default_rng(S)
+    lens = [int(rng.integers(1, longest + 1)) if s % every == every - 1 else 0 for s in range(S)]
+    pool = Pool("bf16", lens, 2, 64, 16, fill=lens)
+    gen = torch.Generator(device=DEV).manual_seed(S)
+    q = _rnd(gen, S, 4, 64, dtype=torch.bfloat16)
+    out, lse, status = _token(pool, q, _i32(lens), 0.125)
+    assert status.item() == 0
+    empty = torch.tensor([n == 0 for n in lens], device=DEV)
+    assert not out[empty].any() and bool(torch.isneginf(lse[empty]).all())
+    some = [s for s, n in enumerate(lens) if n][:60]
+    for s in some + [s for s, n in enumerate(lens) if n][-5:]:
+        ref, ref_lse = oracle.token_attention(_np(q[s]), pool.dense("k", s, lens[s]), pool.dense("v", s, lens[s]), 0.125)
+        tol = HALF_STEP[torch.bfloat16] * np.abs(ref) + 1e-3 * np.abs(pool.dense("v", s, lens[s])).max()
+        assert (np.abs(_np(out[s]) - ref) <= tol).all() and np.abs(lse[s].cpu().numpy() - ref_lse).max() <= 1e-4
+
+
 def test_all_empty_none_and_clamped_lengths():
     pool = Pool("bf16", [64, 64, 64], 2, 64, 16)
     gen = torch.Generator(device=DEV).manual_seed(3)
