@@ -426,16 +426,21 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
     __syncthreads();
   }
   total *= HI;
-  // as many blocks as have a chunk for each of their warps
-  const int most_blocks = max(1, min((int)gridDim.x, (total + NW - 1) / NW));
+  // The chunks of up to 32 sequences are cut item by item, into equal pieces of at most `piece` chunks, one per block: then a block has parts of
+  // one item only and one arrival to wait for, which is worth two chunks and a 32nd, no more.  Where there is little to do a
+  // piece is a chunk for each of the block's warps, and two if that leaves no item to more than one block.  Otherwise, and for more
+  // sequences, the blocks take `each` chunks, the first `more` of them one more, wherever that cuts the items.
+  // (4 items of 256 chunks: 86 blocks that straddle items 12.5 us, 80 that do not 11.3.  8 items of 16 chunks, in 8 blocks instead of 11: 7.5 us
+  // instead of 10.2; 32 items of 8 chunks, in 32 blocks instead of 22: 6.5 instead of 11.1.  A third chunk per warp is not worth it:
+  // 36 chunks 9.5 us in one block, 8.9 in three.)
+  const int n0 = chunks(len0), longest = __reduce_max_sync(full, n0);
+  const int for_warps = a.S <= 32 ? HI * __reduce_add_sync(full, (n0 + NW - 1) / NW) : (total + NW - 1) / NW;
+  const int most_blocks = max(1, min((int)gridDim.x, for_warps));
   const int each = (int)((unsigned)total / (unsigned)most_blocks), more = total - each * most_blocks;
-  // Either the blocks take `each` chunks, the first `more` of them one more, wherever that cuts the items.  Or every item is cut for itself, into
-  // pieces of at most `piece` chunks, one per block: then a block has parts of one item only and one arrival to wait for, which is
-  // worth two chunks and a 32nd, no more.  (4 items of 256 chunks: 86 blocks that straddle items 12.5 us, 80 that do not 11.3.)
-  int x0, x1, item_blocks = 0, in_item = 0;  // of the block's item, in the second case: blocks, and which of them this is
-  const int n0 = chunks(len0);
-  int piece = each + (more > 0), pieces = 0;
+  int x0, x1, item_blocks = 0, in_item = 0;  // of the block's item, if they are cut one by one: blocks, and which of them this is
+  int piece = max(each + (more > 0), NW), pieces = 0;
   if (a.S <= 32 && total > 0) {
+    if (longest <= 2 * NW && HI * __popc(__ballot_sync(full, n0 > 0)) <= most_blocks) piece = longest;
 #pragma unroll 1
     for (int tries = 0; tries < 8; ++tries) {
       pieces = (int)((unsigned)(n0 + piece - 1) / (unsigned)piece);
@@ -445,7 +450,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
         break;
       }
       piece = max(piece + 1, (int)((unsigned)(piece * (int64_t)blocks / most_blocks)));
-      if (piece > each + 2 + each / kAlignSlack) break;
+      if (piece > max(each + 2 + each / kAlignSlack, NW)) break;
     }
   }
   if (item_blocks) {
@@ -1052,7 +1057,9 @@ static int launch_token(const TokenParams& p, cudaStream_t stream) {
   using P = TokenPlan<D, kType, HT>;
   const int64_t most = (int64_t)p.S * p.Hkv * p.tiles * ((p.cache.cap + P::kKeys - 1) / P::kKeys);  // chunks, if every sequence were full
   if (most >= (1 << 30)) return TSD_ERR_UNSUPPORTED;
-  const int64_t grid = std::min<int64_t>(kTokenBlocks, (most + P::kWarps - 1) / P::kWarps);
+  // a chunk for each of a block's warps; up to 32 sequences may be cut item by item
+  const int64_t items = (int64_t)p.S * p.Hkv * p.tiles, per_item = (p.cache.cap + P::kKeys - 1) / P::kKeys;
+  const int64_t grid = std::min<int64_t>(kTokenBlocks, p.S <= 32 ? items * ((per_item + P::kWarps - 1) / P::kWarps) : (most + P::kWarps - 1) / P::kWarps);
   cudaError_t e = allow_smem<D, kType, HT>();
   if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(paged_attention_kernel)");
   e = launch(paged_attention_kernel<D, kType, HT>, dim3((unsigned)std::max<int64_t>(grid, 1)), dim3(P::kWarps * 32), P::kBytes, stream, p);
