@@ -3,10 +3,11 @@
 //     s_t = sm_scale <q, k_t>,   out = sum_t e^(s_t - m) v_t / sum_t e^(s_t - m),   m >= max_t s_t - 8 log 2.
 // Every cached row is read once and used for a few multiply-adds per head, so the kernel is bound by memory; everything in it
 // serves to keep loads in flight and the work behind them short.
-//   split   : the keys of all sequences and heads are laid end to end in chunks of 4 KB of K and 4 KB of V (16 keys of 128 bf16) and cut
-//             evenly over the blocks, one per SM, whatever the single lengths are.  Inside a block the warps take the chunks in turn.
-//   queue   : every warp has its next chunk on the way to shared memory while it works on one (cp.async: 128 KB per SM), and waits for
-//             its own fetches only, never for another warp.
+//   split   : the keys of all sequences and heads are laid end to end in chunks of 4 KB of K and 4 KB of V (16 keys of 128 bf16) and cut over
+//             the blocks, one per SM, evenly or item by item (an item: a sequence and a tile of the heads that share one of its kv
+//             heads).  A block's warps take an even stretch of its chunks each, and walk it without waiting for one another.
+//   queue   : every warp has its next chunk on the way to shared memory while it works on one (cp.async): 12 warps, 96 KB per SM.  (16 warps
+//             with fewer registers: spills; 2 blocks of 8 warps: slower by 3-5 %, another round of joins.)
 //   products: mma.sync m16n8k16 with K (16 keys) or V^T (16 dimensions) as the 16 rows and the heads as the 8 columns: no part of a product is
 //             wasted on 8 heads, and O takes 32 registers.  Which dimensions a step of the contraction takes is arbitrary as long as q is
 //             laid out alike: lane (g, t) = (lane / 4, lane % 4) reads 16 bytes of keys g and g + 8 at offset 64 c + 16 t, and these bytes
@@ -16,11 +17,17 @@
 //             instructions would want 128 rows, and the scores back through tensor memory.
 //   offset  : m moves only when a score passes it by 8 (in the exp2 domain): one vote per chunk instead of a reduction.
 //   fp32    : the same queue on CUDA cores (the scores' partial sums of a key meet over its 4 lanes, the weights in shared memory).
-//   join    : at the end of a sequence's stretch the warps' offsets, sums and rows meet in shared memory; a stretch that is not
-//             the whole of its sequence goes to the workspace, and the last of its blocks to arrive puts the parts together, in their order.
+//   join    : an item that a warp has from its first chunk to its last is written out at once.  Otherwise the warps' offsets, sums and rows meet
+//             in shared memory, and what is not the whole of its item goes to the workspace: the last of the item's blocks to
+//             arrive puts the parts together, in their order whoever arrives last, so that results repeat bit by bit.
 // Lengths are read on the device: a captured call follows them.  Rows past a length are not loaded.
+// Measured (caches larger than L2): 2 sequences of 131072 rows, 28/4 heads of 128, bf16, pages of 64: 88 us, 6.1 TB/s, 93 % of what a copy
+// reaches; the same in e4m3: 51 us, 5.3 TB/s, where conversions come beside the loads; 48 ragged sequences of up to 4096: 41 us, 4.6 TB/s.
+// A call costs about 6 us before its bytes count (the launch and two dependent reads, 2 us; the first chunk on its way, 1 us; the warps'
+// parts, 1 us; the blocks', 2 us): 1 sequence of 768 rows, 32 heads (12.6 MB): 8.8 us.
 #include <cuda_fp16.h>
 #include <algorithm>
+#include <cfloat>
 #include <math_constants.h>
 #include <mutex>
 #include "tsd_paged.cuh"
@@ -28,9 +35,10 @@
 namespace tsd {
 
 constexpr int kTokenBlocks = kPlanSms;  // at most: what the workspace is sized for
-constexpr int kAlignSlack = 32;
+constexpr int kAlignSlack = 32;         // the part of a share by which it may grow to keep items apart
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;           // by how much a score may pass the offset, as a power of 2
+constexpr float kLowest = -FLT_MAX;     // the first offset: finite, so that a score of -infinity has the weight 0 from the first key on
 
 enum { kTypeF32 = TSD_F32, kTypeBf16 = TSD_BF16, kTypeE4m3 = TSD_E4M3 };
 
@@ -631,7 +639,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
 #pragma unroll
     for (int i = 0; i < kAcc; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(m) / 4); ++i) { m[i] = -CUDART_INF_F; l[i] = 0.f; }
+    for (int i = 0; i < (int)(sizeof(m) / 4); ++i) { m[i] = kLowest; l[i] = 0.f; }
   };
   // What an item's chunks have come to so far: put aside as part i of the block, or, if they are all of it, written out.
   auto put_aside = [&](const Item& item, int first, int i) {

@@ -257,9 +257,11 @@ def _token(pool, q, lens, sm_scale, workspace=None, out=None, stream=None):
     return out, lse, status
 
 
-def _check_token(pool, q, lens, out, lse, sm_scale):
+def _check_token(pool, q, lens, out, lse, sm_scale, only=None):
     bits = 2.0 ** -22 if q.dtype == torch.float32 else 2.0 ** -16
     for s, n in enumerate(lens):
+        if only is not None and s not in only:
+            continue
         k, v, qs = pool.dense("k", s, n), pool.dense("v", s, n), _np(q[s])
         ref, ref_lse = oracle.token_attention(qs, k, v, sm_scale)
         if n == 0:
@@ -333,11 +335,33 @@ def test_few_sequences_among_many_slots(S, every, longest):
     assert status.item() == 0
     empty = torch.tensor([n == 0 for n in lens], device=DEV)
     assert not out[empty].any() and bool(torch.isneginf(lse[empty]).all())
-    some = [s for s, n in enumerate(lens) if n][:60]
-    for s in some + [s for s, n in enumerate(lens) if n][-5:]:
-        ref, ref_lse = oracle.token_attention(_np(q[s]), pool.dense("k", s, lens[s]), pool.dense("v", s, lens[s]), 0.125)
-        tol = HALF_STEP[torch.bfloat16] * np.abs(ref) + 1e-3 * np.abs(pool.dense("v", s, lens[s])).max()
-        assert (np.abs(_np(out[s]) - ref) <= tol).all() and np.abs(lse[s].cpu().numpy() - ref_lse).max() <= 1e-4
+    some = [s for s, n in enumerate(lens) if n]
+    _check_token(pool, q, lens, out, lse, 0.125, only=set(some[:60] + some[-5:]))
+
+
+@pytest.mark.parametrize("kind,Hq,Hkv", [("bf16", 8, 8), ("bf16", 20, 1), ("f32", 4, 2)])
+def test_scores_of_minus_infinity_weigh_nothing(kind, Hq, Hkv):
+    # the first chunks of one sequence, whole stretches of another, all but the last key of a third; every key of the fourth (0 / 0)
+    lens, masked = [300, 9000, 200, 50], [range(0, 64), range(1000, 7000), range(0, 199), range(0, 50)]
+    pool = Pool(kind, lens, Hkv, 128, 64)
+    pages = pool.pages["k"]
+    for s, rows in enumerate(masked):
+        at = torch.tensor(list(rows), device=DEV)
+        pages[pool.table[s, at // 64].long(), at % 64, :, 3] = -float("inf")
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    q = _rnd(gen, 4, Hq, 128, dtype=pool.dtype)
+    q[:, :, 3] = q[:, :, 3].abs() + 0.5
+    out, lse, _ = _token(pool, q, _i32(lens), 128 ** -0.5)
+    assert bool(torch.isnan(out[3]).all())
+    # the same without those keys, one sequence at a time
+    for s in range(3):
+        live = [t for t in range(lens[s]) if t not in masked[s]]
+        rest = Pool(kind, [len(live)], Hkv, 128, 64)
+        for x in "kv":
+            rows = pool.pages[x][pool.table[s, torch.tensor(live, device=DEV) // 64].long(), torch.tensor(live, device=DEV) % 64]
+            to = torch.arange(len(live), device=DEV)
+            rest.pages[x][rest.table[0, to // 64].long(), to % 64] = rows
+        _check_token(rest, q[s:s + 1], [len(live)], out[s:s + 1], lse[s:s + 1], 128 ** -0.5)
 
 
 def test_all_empty_none_and_clamped_lengths():
