@@ -35,7 +35,7 @@
 namespace tsd {
 
 constexpr int kTokenBlocks = kPlanSms;  // at most: what the workspace is sized for
-constexpr int kAlignSlack = 32;         // the part of a share by which it may grow to keep items apart
+constexpr int kAlignSlack = 4;          // the part of a share by which it may grow to keep items apart
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;           // by how much a score may pass the offset, as a power of 2
 constexpr float kLowest = -FLT_MAX;     // the first offset: finite, so that a score of -infinity has the weight 0 from the first key on
@@ -434,31 +434,38 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
     __syncthreads();
   }
   total *= HI;
-  // The chunks of up to 32 sequences are cut item by item, into equal pieces of at most `piece` chunks, one per block: then a block has parts of
-  // one item only and one arrival to wait for, which is worth two chunks and a 32nd, no more.  Where there is little to do a
-  // piece is a chunk for each of the block's warps, and two if that leaves no item to more than one block.  Otherwise, and for more
-  // sequences, the blocks take `each` chunks, the first `more` of them one more, wherever that cuts the items.
-  // (4 items of 256 chunks: 86 blocks that straddle items 12.5 us, 80 that do not 11.3.  8 items of 16 chunks, in 8 blocks instead of 11: 7.5 us
-  // instead of 10.2; 32 items of 8 chunks, in 32 blocks instead of 22: 6.5 instead of 11.1.  A third chunk per warp is not worth it:
-  // 36 chunks 9.5 us in one block, 8.9 in three.)
+  // The chunks of up to 32 sequences are cut item by item, into equal pieces, one per block: then a block has parts of one item only and one
+  // arrival to wait for, and fewer blocks than SMs have the memory's rate too.  That is worth pieces a quarter longer than an
+  // even share.  Where there is little to do a piece is a chunk for each of the block's warps, and two if that leaves no item to
+  // more than one block.  Otherwise, and for more sequences, the blocks take `each` chunks, the first `more` of them one more, wherever
+  // that cuts the items.  (16 sequences of 2048, 8 kv heads, in 128 blocks instead of 148: 27.4 us instead of 30.8; 120 heads of one sequence
+  // of 8192 in 120: 78.2, 82.5; with pieces a half longer 50 heads in 100 blocks 73.6, 72.1, in e4m3 50.4, 44.0.  8 items of 16 chunks, in
+  // 8 blocks instead of 11: 7.5 us instead of 10.2; 32 items of 8 chunks, in 32 blocks instead of 22: 6.5 instead of 11.1.  A third chunk
+  // per warp is not worth it: 36 chunks 9.5 us in one block, 8.9 in three.)
   const int n0 = chunks(len0), longest = __reduce_max_sync(full, n0);
   const int for_warps = a.S <= 32 ? HI * __reduce_add_sync(full, (n0 + NW - 1) / NW) : (total + NW - 1) / NW;
   const int most_blocks = max(1, min((int)gridDim.x, for_warps));
   const int each = (int)((unsigned)total / (unsigned)most_blocks), more = total - each * most_blocks;
   int x0, x1, item_blocks = 0, in_item = 0;  // of the block's item, if they are cut one by one: blocks, and which of them this is
-  int piece = max(each + (more > 0), NW), pieces = 0;
+  int pieces = 0;                         // of each item of the lane's sequence
   if (a.S <= 32 && total > 0) {
-    if (longest <= 2 * NW && HI * __popc(__ballot_sync(full, n0 > 0)) <= most_blocks) piece = longest;
+    auto fit = [&](int piece) {  // a quotient that is off by a rounding is as good: what counts is the pieces' number
+      pieces = n0 > 0 ? max(1, (int)ceilf(__fdividef((float)n0, (float)piece))) : 0;
+      return HI * __reduce_add_sync(full, pieces) <= most_blocks;
+    };
+    int lo = each + (more > 0) - 1, hi = each + 2 + each / kAlignSlack;  // the smallest that fits is looked for in (lo, hi]
+    if (for_warps == most_blocks) { hi = NW; lo = hi - 1; }
+    if (longest <= 2 * NW && HI * __popc(__ballot_sync(full, n0 > 0)) <= most_blocks) { hi = longest; lo = hi - 1; }
+    if (fit(hi)) {
+      item_blocks = 1;
+      int best = pieces;
 #pragma unroll 1
-    for (int tries = 0; tries < 8; ++tries) {
-      pieces = (int)((unsigned)(n0 + piece - 1) / (unsigned)piece);
-      const int blocks = __reduce_add_sync(full, pieces) * HI;
-      if (blocks <= most_blocks) {
-        item_blocks = 1;
-        break;
+      for (int tries = 0; tries < 5 && lo + 1 < hi; ++tries) {
+        const int mid = (lo + hi) >> 1;
+        if (fit(mid)) { hi = mid; best = pieces; }
+        else lo = mid;
       }
-      piece = max(piece + 1, (int)((unsigned)(piece * (int64_t)blocks / most_blocks)));
-      if (piece > max(each + 2 + each / kAlignSlack, NW)) break;
+      pieces = best;
     }
   }
   if (item_blocks) {
