@@ -21,10 +21,10 @@
 //             in shared memory, and what is not the whole of its item goes to the workspace: the last of the item's blocks to
 //             arrive puts the parts together, in their order whoever arrives last, so that results repeat bit by bit.
 // Lengths are read on the device: a captured call follows them.  Rows past a length are not loaded.
-// Measured (caches larger than L2): 2 sequences of 131072 rows, 28/4 heads of 128, bf16, pages of 64: 88 us, 6.1 TB/s, 93 % of what a copy
-// reaches; the same in e4m3: 51 us, 5.3 TB/s, where conversions come beside the loads; 48 ragged sequences of up to 4096: 41 us, 4.6 TB/s.
-// A call costs about 6 us before its bytes count (the launch and two dependent reads, 2 us; the first chunk on its way, 1 us; the warps'
-// parts, 1 us; the blocks', 2 us): 1 sequence of 768 rows, 32 heads (12.6 MB): 8.8 us.
+// Measured (caches larger than L2): 2 sequences of 131072 rows, 28/4 heads of 128, bf16, pages of 64: 85.7 us, 6.27 TB/s, 95 % of what a copy
+// reaches; the same in e4m3: 50.3 us, 5.3 TB/s, where conversions come beside the loads; 48 ragged sequences of up to 4096: 39.9 us, 4.8
+// TB/s.  A call costs about 6 us before its bytes count (the launch and two dependent reads, 2 us; the first chunk on its way, 1 us; the
+// warps' parts, 1 us; the blocks', 2 us): 1 sequence of 768 rows, 32 heads (12.6 MB): 8.9 us.
 #include <cuda_fp16.h>
 #include <algorithm>
 #include <cfloat>
@@ -36,6 +36,7 @@ namespace tsd {
 
 constexpr int kTokenBlocks = kPlanSms;  // at most: what the workspace is sized for
 constexpr int kAlignSlack = 4;          // the part of a share by which it may grow to keep items apart
+constexpr int kReadPast = 4096;         // chunks: 32 MB, a quarter of L2
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;           // by how much a score may pass the offset, as a power of 2
 constexpr float kLowest = -FLT_MAX;     // the first offset: finite, so that a score of -infinity has the weight 0 from the first key on
@@ -98,9 +99,9 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t& pair, uin
     rest = bf16_pair(x - __uint_as_float(pair << 16), y - __uint_as_float(pair & 0xffff0000u));
   }
 }
-// 16 bytes of the cache, or zeros, into shared memory, asynchronously.
-__device__ __forceinline__ void fetch16(uint32_t to, const uint8_t* p, bool wanted) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(p), "r"(wanted ? 16 : 0) : "memory");
+// 16 bytes of the cache, or zeros, into shared memory, asynchronously; `policy`: what L2 is to do with their line.
+__device__ __forceinline__ void fetch16(uint32_t to, const uint8_t* p, bool wanted, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(to), "l"(p), "r"(wanted ? 16 : 0), "l"(policy) : "memory");
 }
 __device__ __forceinline__ void fetch_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -566,6 +567,11 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
   const uint32_t queue_at = (uint32_t)__cvta_generic_to_shared(queue);
   const int64_t lane_from = my_row * row_bytes + 16 * my_piece;
   // `at`: lane i < NG, where the chunk's 8 keys from 8 i on begin (from k or v on), -1 where there is no page; `left`: how many keys count
+  // Much data is read past what else L2 holds, the code of what follows the loop above all: 0.8-2 us per call.  Data that may still be there
+  // from the call before is left to it (12.6 MB, read again and again: 8.8 us, read past it 9.6).
+  uint64_t policy;
+  if (total >= kReadPast) asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+  else asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
   auto fetch = [&](int64_t at, int left, const void* pages, uint32_t to) {
 #pragma unroll
     for (int nb = 0; nb < NG; ++nb) {
@@ -575,7 +581,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged
 #pragma unroll
       for (int j = 0; j < 8 / kRowsAtOnce; ++j) {
         const int row0 = 8 * nb + j * kRowsAtOnce;
-        fetch16(to + (lane_to ^ (swizzle(row0) * 16)) + row0 * P::kRow, p, j * kRowsAtOnce < here);
+        fetch16(to + (lane_to ^ (swizzle(row0) * 16)) + row0 * P::kRow, p, j * kRowsAtOnce < here, policy);
         p += kRowsAtOnce * row_bytes;
       }
     }
