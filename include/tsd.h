@@ -625,7 +625,7 @@ int tsd_wait_block(int32_t batch, const uint64_t* report, uint32_t ticket, int32
  *   page_table   device int32 [batch, max_pages], sequences table_stride entries apart.  Only the entries of
  *                tokens that a call reads or writes are looked at.  One of those outside [0, n_pages) sets
  *                TSD_STATUS_BAD_INDEX: its tokens are not written, and read as rows of zeros.
- *   page_size    8, 16, 32, ... 1024;  max_pages * page_size < 2^31.
+ *   page_size    8, 16, 32, ... 1024;  max_pages * page_size at most 2^31 - 1024.
  *   head_dim     64 or 128;  dtype TSD_F32, TSD_BF16 or TSD_E4M3 (with queries, new rows and outputs in bf16).
  * Pages may be shared by sequences that only read them.
  * ------------------------------------------------------------------------- */
@@ -657,7 +657,7 @@ typedef struct {
  *                What belongs to the others, in the cache and in q_out and k_out, is left as it was.
  *   first_slot   device int32 [batch], nullable (= 0);  positions device int32 [batch, n_rows], nullable.
  *   inv_freq     device fp32 [rotary_dim / 2];  rotary_dim a multiple of 16, 0 (no rotation) to head_dim.
- * All bases 16-byte aligned, strides multiples of 16 bytes.  A block outside [0, n_blocks) sets TSD_STATUS_BAD_INDEX
+ * All bases 16-byte aligned, strides multiples of 16 bytes; those of q_out and k_out at least head_dim.  A block outside [0, n_blocks) sets TSD_STATUS_BAD_INDEX
  * and leaves that sequence unwritten; so does a slot outside the cache, for that row of the cache.  Two rows that
  * go to one slot (sequences that share the page) leave it with the bytes of either.
  * ------------------------------------------------------------------------- */
@@ -682,7 +682,7 @@ int tsd_append_paged_kv(const tsd_append_args* args, tsd_stream_t stream);
  * of length 0 gives 0 and a log-sum-exp of -inf.  Rows at or past kv_lens[s] can hold anything.
  *
  *   q, out     device [batch, n_q_heads, head_dim] of `dtype` (TSD_F32 with an fp32 cache, else TSD_BF16), strides
- *              (batch, head); 16-byte aligned bases and strides.
+ *              (batch, head); 16-byte aligned bases and strides, those of out at least head_dim.
  *   kv_lens    device int32 [batch], nullable (= max_pages * page_size), clamped to that.
  *   lse        device fp32 [batch, n_q_heads], nullable: natural-log sum-exp of the scaled scores.
  *   workspace  device, 16-byte aligned, tsd_paged_attention_workspace_bytes() bytes: parts of sequences that

@@ -22,7 +22,8 @@ int check_paged_cache(const tsd_paged_cache* c) {
   if (c->batch < 1 || c->n_pages < 1 || c->max_pages < 1 || c->n_kv_heads < 1 || c->table_stride < 0) return TSD_ERR_INVALID_ARG;
   if (c->page_size < 1) return TSD_ERR_INVALID_ARG;
   if (c->page_size < 8 || c->page_size > 1024 || (c->page_size & (c->page_size - 1))) return TSD_ERR_UNSUPPORTED;
-  if ((int64_t)c->max_pages * c->page_size > 0x7fffffffll) return TSD_ERR_INVALID_ARG;
+  // room behind the last token for the kernels to count on to the end of a tile
+  if ((int64_t)c->max_pages * c->page_size > 0x80000000ll - 1024) return TSD_ERR_INVALID_ARG;
   if (c->batch > 1 && c->table_stride < c->max_pages) return TSD_ERR_INVALID_ARG;
   if (c->head_dim != 64 && c->head_dim != 128) return TSD_ERR_UNSUPPORTED;
   if (c->dtype != TSD_F32 && c->dtype != TSD_BF16 && c->dtype != TSD_E4M3) return TSD_ERR_UNSUPPORTED;
@@ -110,7 +111,7 @@ __device__ __forceinline__ void store_cached(uint8_t* p, const float (&x)[8], fl
 
 // cos and sin of position * inv_freq.  t = the angle in turns; q = its nearest quarter; the rest, at most an eighth of a turn, is
 // small enough that fp32 holds it to 5e-8 of a radian.
-__device__ __forceinline__ float2 cos_sin(int position, float inv_freq) {
+__device__ __forceinline__ float2 cos_sin(int64_t position, float inv_freq) {
   const double t = (double)position * (double)inv_freq * 0.15915494309189533577;
   const double quarter = rint(t * 4.0);
   const float rest = (float)fma(quarter, -0.25, t);
@@ -236,7 +237,7 @@ append_kernel(const T* k, const T* v, const T* q, T* k_out, T* q_out, AppendPara
     }
     float2 turn[8];
     if (half > 0) {
-      const int position = p.positions ? p.positions[s * (int64_t)p.n_rows + task.row.i] : (int)slot;
+      const int64_t position = p.positions ? p.positions[s * (int64_t)p.n_rows + task.row.i] : slot;
       __syncwarp();
 #pragma unroll 1
       for (int j = lane; j < half; j += 32) turns[warp][j] = cos_sin(position, p.inv_freq[j]);
@@ -317,9 +318,9 @@ static cudaError_t launch_append(const tsd_append_args& a, const AppendParams& p
   return a.head_dim == 64 ? launch_append<T, C, 64>(a, p, stream) : launch_append<T, C, 128>(a, p, stream);
 }
 
-// Strides (batch, row, head) of rows of heads; a dimension of size 1 may have any.
-static bool strides_ok(const int64_t (&st)[3], int batch, int64_t rows, int heads, int head_dim, int esize) {
-  const int64_t counts[3] = {batch, rows, heads}, least[3] = {0, 0, head_dim};
+// Strides (batch, row, head) of rows of heads; a dimension of size 1 may have any.  What is only read may be the same for all sequences or rows.
+static bool strides_ok(const int64_t (&st)[3], int batch, int64_t rows, int heads, int head_dim, int esize, bool written) {
+  const int64_t counts[3] = {batch, rows, heads}, each = written ? head_dim : 0, least[3] = {each, each, head_dim};
   for (int i = 0; i < 3; ++i)
     if (counts[i] > 1 && (st[i] < least[i] || (st[i] * esize) % 16 != 0)) return false;
   return true;
@@ -344,12 +345,12 @@ static int check_append(const tsd_append_args& a) {
     if (ptr && !aligned16(ptr)) return TSD_ERR_INVALID_ARG;
   const int64_t rows = (int64_t)a.n_blocks * a.n_rows;
   const int esize = a.dtype == TSD_F32 ? 4 : 2;
-  if (!strides_ok(a.kv_stride, a.batch, rows, a.n_kv_heads, a.head_dim, esize)) return TSD_ERR_INVALID_ARG;
-  if (a.k_out && !strides_ok(a.k_out_stride, a.batch, rows, a.n_kv_heads, a.head_dim, esize)) return TSD_ERR_INVALID_ARG;
-  if (a.q && (!strides_ok(a.q_stride, a.batch, rows, a.n_q_heads, a.head_dim, esize) ||
-              !strides_ok(a.q_out_stride, a.batch, rows, a.n_q_heads, a.head_dim, esize)))
+  if (!strides_ok(a.kv_stride, a.batch, rows, a.n_kv_heads, a.head_dim, esize, false)) return TSD_ERR_INVALID_ARG;
+  if (a.k_out && !strides_ok(a.k_out_stride, a.batch, rows, a.n_kv_heads, a.head_dim, esize, true)) return TSD_ERR_INVALID_ARG;
+  if (a.q && (!strides_ok(a.q_stride, a.batch, rows, a.n_q_heads, a.head_dim, esize, false) ||
+              !strides_ok(a.q_out_stride, a.batch, rows, a.n_q_heads, a.head_dim, esize, true)))
     return TSD_ERR_INVALID_ARG;
-  if (a.n_q_heads > (1 << 20) || a.n_kv_heads > (1 << 20) || (int64_t)a.batch * a.n_rows > 0x7fffffffll || rows > 0x7fffffffll)
+  if (a.n_q_heads > (1 << 20) || a.n_kv_heads > (1 << 20) || (int64_t)a.batch * a.n_rows > 0x7ff00000ll || rows > 0x7fffffffll)
     return TSD_ERR_UNSUPPORTED;
   return TSD_OK;
 }

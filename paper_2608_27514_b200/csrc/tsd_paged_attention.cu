@@ -1120,7 +1120,7 @@ int tsd_paged_attention(const tsd_paged_cache* c, int32_t n_q_heads, int32_t dty
   const int esize = dtype == TSD_F32 ? 4 : 2;
   const int64_t strides[4] = {q_stride_b, o_stride_b, q_stride_head, o_stride_head};
   for (int i = 0; i < 4; ++i)
-    if ((i < 2 ? c->batch : n_q_heads) > 1 && (strides[i] < (i < 2 ? 0 : c->head_dim) || (strides[i] * esize) % 16 != 0))
+    if ((i < 2 ? c->batch : n_q_heads) > 1 && (strides[i] < (i == 0 ? 0 : c->head_dim) || (strides[i] * esize) % 16 != 0))
       return TSD_ERR_INVALID_ARG;
   if (workspace_bytes < tsd_paged_attention_workspace_bytes(c, n_q_heads)) return TSD_ERR_WORKSPACE;
   tsd::TokenParams p = {};

@@ -186,6 +186,17 @@ def test_far_and_negative_positions(interleaved):
     assert (np.abs(_np(out) - ref) <= tol).all()
 
 
+def test_positions_counted_on_beyond_31_bits():
+    # rotated only, so that no slot has to exist: the second row stands at 2^31
+    gen = torch.Generator(device=DEV).manual_seed(10)
+    k = _rnd(gen, 1, 2, 2, 64)
+    freq = 2.0 ** -torch.arange(20, 28, device=DEV).float()
+    out = torch.empty_like(k)
+    B.tsd_append_paged_kv(None, k, None, _i32([0x7fffffff]), inv_freq=freq, k_out=out)
+    ref = oracle.rotate(_np(k), np.array([[0x7fffffff, 0x80000000]]), _np(freq))
+    assert (np.abs(_np(out) - ref) <= 2.0 ** -24 * np.abs(ref) + 3e-7 * _pair_size(_np(k), 8, False) + 1e-30).all()
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 def test_the_accepted_block_goes_to_its_pages(kind):
     # the rows of one node of many, unrotated, the same bytes that the hand-over into a dense cache gives; views with other strides

@@ -149,3 +149,16 @@ def test_descriptions_of_host_tensors_are_refused(lib):
     pages = torch.zeros((4, 8, 2, 64), dtype=torch.bfloat16)
     with pytest.raises(ValueError):
         B.make_paged_cache(pages, pages, torch.zeros((1, 4), dtype=torch.int32))
+
+
+def test_results_that_would_meet_and_sizes_at_the_limit(lib):
+    # a stride of 0 is for what is read only; the largest cache leaves the kernels room to count behind its last token
+    bad = B.TSD_ERR_INVALID_ARG
+    assert token(lib, cache(), ob=0) == bad and token(lib, cache(), ob=64) == bad
+    for kw in (dict(q_out_stride=(0, 3584, 128)), dict(q_out_stride=(96 * 3584, 0, 128)), dict(k_out=P, k_out_stride=(96 * 512, 0, 128))):
+        assert append(lib, **kw) == bad, kw
+    need = lambda **kw: lib.tsd_paged_attention_workspace_bytes(ctypes.byref(cache(**kw)), 28)
+    assert need(page_size=1024, max_pages=(1 << 21) - 1, table_stride=1 << 21) > 0
+    assert need(page_size=1024, max_pages=1 << 21, table_stride=1 << 21) == 0
+    assert need(page_size=8, max_pages=(1 << 28) - 128, table_stride=1 << 28) > 0
+    assert need(page_size=8, max_pages=(1 << 28) - 127, table_stride=1 << 28) == 0
