@@ -199,7 +199,8 @@ __device__ __noinline__ void join_parts(const TokenParams& p, uint8_t* dynamic, 
   constexpr int NW = P::kWarps;
   constexpr bool kF32 = kType == kTypeF32, kF16 = kType == kTypeE4m3;
   constexpr unsigned full = 0xffffffffu;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, x0 = sh.x0, x1 = sh.x1, each = sh.each, more = sh.more;
+  // the shuffle tells the compiler that the warp branches together, a third of this function's code
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, x0 = sh.x0, x1 = sh.x1, each = sh.each, more = sh.more;
   auto& part_m = sh.part_m;
   auto& part_l = sh.part_l;
   auto& part_item = sh.part_item;
@@ -332,40 +333,37 @@ __device__ __noinline__ void join_parts(const TokenParams& p, uint8_t* dynamic, 
         for (int i0 = sub; i0 < n_parts; i0 += 32 * subs) {
           const int i = i0 + lane * subs;
           const bool in = i < n_parts;
-          float4 v[8];
-          auto take = [&](int j) {  // parts j .. j + 7 of the 32
+          const float mine = in ? __ldcg(part_at(i) + HT * D + row) : -CUDART_INF_F;
+          const float sum_mine = in ? __ldcg(part_at(i) + HT * D + HT + row) : 0.f;
+          float weight = 0.f;
+#pragma unroll 1
+          for (int j = 0; j < 32 && i0 + j * subs < n_parts; j += 8) {
+            float4 v[8];
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
               const int k = i0 + (j + u) * subs;
               v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
               if (k < n_parts) v[u] = __ldcg(reinterpret_cast<const float4*>(part_at(k) + col));
             }
-          };
-          const float mine = in ? __ldcg(part_at(i) + HT * D + row) : -CUDART_INF_F;
-          const float sum_mine = in ? __ldcg(part_at(i) + HT * D + HT + row) : 0.f;
-          int j = 0;
-          take(0);
-          float to = mine;
+            if (j == 0) {
+              float to = mine;
 #pragma unroll
-          for (int off = 16; off >= 1; off >>= 1) to = fmaxf(to, __shfl_xor_sync(full, to, off));
-          to = fmaxf(to, top);
-          const float alpha = top == to ? 1.f : exp2_approx(top - to), weight = in ? exp2_approx(mine - to) : 0.f;
-          top = to;
-          float all = sum_mine * weight;
+              for (int off = 16; off >= 1; off >>= 1) to = fmaxf(to, __shfl_xor_sync(full, to, off));
+              to = fmaxf(to, top);
+              const float alpha = top == to ? 1.f : exp2_approx(top - to);
+              weight = in ? exp2_approx(mine - to) : 0.f;
+              top = to;
+              float all = sum_mine * weight;
 #pragma unroll
-          for (int off = 16; off >= 1; off >>= 1) all += __shfl_xor_sync(full, all, off);
-          sum = fmaf(sum, alpha, all);
-          o.x *= alpha; o.y *= alpha; o.z *= alpha; o.w *= alpha;
-#pragma unroll 1
-          while (true) {
+              for (int off = 16; off >= 1; off >>= 1) all += __shfl_xor_sync(full, all, off);
+              sum = fmaf(sum, alpha, all);
+              o.x *= alpha; o.y *= alpha; o.z *= alpha; o.w *= alpha;
+            }
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-              const float f = __shfl_sync(full, weight, j + u);  // 0 behind the last
+              const float f = __shfl_sync(full, weight, j + u);
               o.x = fmaf(v[u].x, f, o.x); o.y = fmaf(v[u].y, f, o.y); o.z = fmaf(v[u].z, f, o.z); o.w = fmaf(v[u].w, f, o.w);
             }
-            j += 8;
-            if (j == 32 || i0 + j * subs >= n_parts) break;
-            take(j);
           }
         }
         if (subs == 1) {
