@@ -680,6 +680,7 @@ int tsd_append_paged_kv(const tsd_append_args* args, tsd_stream_t stream);
  *     out[s, h] = sum_t softmax_t(sm_scale * <q[s, h], k_t>) v_t ,  t < kv_lens[s],
  * kv head h / (n_q_heads / n_kv_heads).  The new token's own key and value are in the cache already.  A sequence
  * of length 0 gives 0 and a log-sum-exp of -inf.  Rows at or past kv_lens[s] can hold anything.
+ * Of the rows before: a score of -infinity weighs nothing; a value that is not finite makes its dimension of the heads that read it NaN.
  *
  *   q, out     device [batch, n_q_heads, head_dim] of `dtype` (TSD_F32 with an fp32 cache, else TSD_BF16), strides
  *              (batch, head); 16-byte aligned bases and strides, those of out at least head_dim.

@@ -9,7 +9,7 @@
 // around the nearest quarter (a position of 10^6 leaves 1e-10 of an angle there; in fp32 it would leave 0.1), then sine and cosine in
 // fp32, two per lane and handed on through shared memory.
 // Bound by memory: each row is read once and written once, and nothing but the tables comes on top.  Measured (cold): 16 prompts of 1504 rows,
-// 32 heads of 128, q rotated in the same pass: 206 us, 5.7 TB/s, 88 % of what a copy reaches; 4206 rows of 4 heads into e4m3 pages
+// 32 heads of 128, q rotated in the same pass: 206 us, 5.7 TB/s, 88 % of what a copy reaches; 1845 rows of 4 heads into e4m3 pages
 // and 28 heads of q: 8.6 us, 3.7 TB/s; one row for each of 8 sequences: 3.8 us, of which the launch is most.
 #include <cuda_fp8.h>
 #include <algorithm>
@@ -201,7 +201,7 @@ append_kernel(const T* k, const T* v, const T* q, T* k_out, T* q_out, AppendPara
   Task task = ahead;
   int slot_in = 0, slot_out = 0;
   const uint32_t queue_at = (uint32_t)__cvta_generic_to_shared(&queue[warp][0][0][lane]);
-  // What has been read leaves L2 before what is written, which attention wants next.  (1.2 GB 215 -> 206 us, 4206 rows into e4m3 pages 9.3 -> 8.6;
+  // What has been read leaves L2 before what is written, which attention wants next.  (1.2 GB 215 -> 206 us, 1845 rows into e4m3 pages 9.3 -> 8.6;
   // 0.44 GB 72.0 -> 73.4.)
   uint64_t read_once;
   asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(read_once));
