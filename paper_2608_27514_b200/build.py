@@ -1,5 +1,6 @@
 """Builds libtsd.so (the C-ABI CUDA library) with nvcc for sm_100a, and _tsd_native.so (its Python side), in-tree."""
 import glob
+import importlib.util
 import os
 import subprocess
 import sys
@@ -54,9 +55,10 @@ def build(force=False, verbose=False):
     tmp = LIB + ".%d.tmp" % os.getpid()
     subprocess.check_call([NVCC, "-shared", "-o", tmp] + objs + ["-gencode", "arch=compute_100a,code=sm_100a"])
     os.replace(tmp, LIB)
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]  # for the header of its exchange table; not linked
     tmp = NATIVE + ".%d.tmp" % os.getpid()
-    subprocess.check_call(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I" + sysconfig.get_paths()["include"], NATIVE_SRC,
-                           "-o", tmp, "-L" + HERE, "-l:libtsd.so", "-Wl,-rpath,$ORIGIN"])
+    subprocess.check_call(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I" + sysconfig.get_paths()["include"],
+                           "-I" + os.path.join(torch, "include"), NATIVE_SRC, "-o", tmp, "-L" + HERE, "-l:libtsd.so", "-Wl,-rpath,$ORIGIN"])
     os.replace(tmp, NATIVE)
     return LIB
 

@@ -1,16 +1,20 @@
 // Python side of the C ABI for the calls that a decode loop makes on every pass: takes torch tensors, reads their
 // addresses and strides, calls libtsd.  A call through ctypes costs 10-17 us of interpreter time (argument
 // conversion, torch.cuda.current_stream()), as much as the kernels of a small pass; here it costs about 2 us plus
-// the launches.  Only the CPython API is used: tensors are asked for data_ptr(), stride(), shape and nbytes.
+// the launches.  Only the CPython API is used: tensors are asked for data_ptr(), stride(), shape and nbytes, or (the calls on
+// a paged cache) for all of it at once through torch's DLPack exchange table, a C interface.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <stdint.h>
+#include <type_traits>
+#include <ATen/dlpack.h>
 #include "../../include/tsd.h"
 
 namespace {
 
-PyObject *n_data_ptr, *n_stride, *n_shape, *n_nbytes, *n_dtype, *n_cuda_stream, *n_is_contiguous, *n_get_device, *n_device;
-PyObject *get_device, *get_raw_stream, *dtype_f32, *dtype_bf16, *dtype_i32, *error_type;  // set by setup()
+PyObject *n_data_ptr, *n_stride, *n_shape, *n_nbytes, *n_dtype, *n_cuda_stream, *n_is_contiguous, *n_device;
+PyObject *get_device, *get_raw_stream, *dtype_f32, *dtype_bf16, *error_type, *tensor_type;  // set by setup()
+const DLPackExchangeAPI* exchange;
 
 struct Failed {};  // a Python exception is set
 
@@ -144,7 +148,15 @@ PyObject* done(int rc, const char* where) {
 using Args = PyObject* const*;
 
 PyObject* setup(Args a) {
-  PyObject** to[] = {&get_device, &get_raw_stream, &dtype_f32, &dtype_bf16, &dtype_i32, &error_type};
+  const void* table = PyCapsule_GetPointer(a[6], "dlpack_exchange_api");
+  if (!table) throw Failed{};
+  const auto* api = static_cast<const DLPackExchangeAPI*>(table);
+  if (api->header.version.major != DLPACK_MAJOR_VERSION || !api->dltensor_from_py_object_no_sync) {
+    PyErr_SetString(PyExc_RuntimeError, "torch's DLPack exchange table is of another version than the one this was built with");
+    throw Failed{};
+  }
+  exchange = api;
+  PyObject** to[] = {&get_device, &get_raw_stream, &dtype_f32, &dtype_bf16, &error_type, &tensor_type};
   for (int i = 0; i < 6; ++i) {
     Py_INCREF(a[i]);
     Py_XSETREF(*to[i], a[i]);
@@ -400,16 +412,51 @@ PyObject* advance_block(Args a) {
 
 // ---- the calls on a paged cache check what they are given: sizes, types, and that it lies on the current device
 struct Here {
-  int64_t device;
+  int32_t device;
   Here() {
     Ref d(PyObject_CallNoArgs(get_device));
-    device = to_int(d.p);
+    device = to_i32(d.p);
   }
-  void operator()(PyObject* t) const {  // None is fine
-    if (t == Py_None) return;
-    Ref d(PyObject_CallMethodNoArgs(t, n_get_device));
-    want(to_int(d.p) == device, "tensors lie on the current CUDA device");
+  tsd_stream_t stream(PyObject* s) const {  // None = torch's current one
+    if (s != Py_None) return stream_of(s);
+    void* raw = nullptr;
+    if (exchange->current_work_stream(kDLCUDA, device, &raw)) throw Failed{};
+    return reinterpret_cast<tsd_stream_t>(raw);
   }
+};
+// A tensor's address, sizes, strides, type and device, read at once: 30 ns, where attributes and methods take 300.
+struct Tensor {
+  DLTensor t = {};
+  Tensor(PyObject* o, const Here& here) {
+    if (!PyObject_TypeCheck(o, reinterpret_cast<PyTypeObject*>(tensor_type))) {
+      PyErr_SetString(PyExc_TypeError, "a tensor is wanted");
+      throw Failed{};
+    }
+    if (exchange->dltensor_from_py_object_no_sync(o, &t)) throw Failed{};
+    want(t.device.device_type == kDLCUDA && t.device.device_id == here.device, "tensors lie on the current CUDA device");
+  }
+  bool is(uint8_t code, uint8_t bits) const { return t.dtype.code == code && t.dtype.bits == bits && t.dtype.lanes == 1; }
+  int64_t count() const {
+    int64_t n = 1;
+    for (int i = 0; i < t.ndim; ++i) n *= t.shape[i];
+    return n;
+  }
+  bool contiguous() const {  // as torch has it: the stride of a dimension of size 1 does not matter
+    int64_t n = 1;
+    for (int i = t.ndim - 1; i >= 0; --i) {
+      if (t.shape[i] == 0) return true;
+      if (t.shape[i] != 1 && t.strides && t.strides[i] != n) return false;
+      n *= t.shape[i];
+    }
+    return true;
+  }
+  void* data() const { return static_cast<char*>(t.data) + t.byte_offset; }
+  template <int N>
+  void sizes(int64_t (&n)[N], int64_t (&st)[N], const char* what) const {
+    want(t.ndim == N && t.strides, what);
+    for (int i = 0; i < N; ++i) { n[i] = t.shape[i]; st[i] = t.strides[i]; }
+  }
+  int32_t model_type(PyObject* o) const { return is(kDLBfloat, 16) ? (int32_t)TSD_BF16 : is(kDLFloat, 32) ? (int32_t)TSD_F32 : dtype_code(o); }
 };
 struct Pages : Structure<tsd_paged_cache> {
   Pages(PyObject* o, const Here& here) : Structure(o, "a tsd_paged_cache is wanted") {
@@ -417,28 +464,31 @@ struct Pages : Structure<tsd_paged_cache> {
     want(to_int(d.p) == here.device, "the cache lies on the current CUDA device");
   }
 };
-void typed(PyObject* t, PyObject* dtype, const char* what) {
-  Ref d(PyObject_GetAttr(t, n_dtype));
-  want(d.p == dtype, what);
-}
 // contiguous int32 (fp32) of `count` elements, or None
 template <typename T>
-T* vec(PyObject* t, PyObject* dtype, int64_t count, const Here& here, const char* what) {
-  if (t == Py_None) return nullptr;
-  here(t);
-  typed(t, dtype, what);
-  want(contiguous(t) && (int64_t)nbytes(t) == count * 4, what);
-  return ptr<T>(t);
+T* vec(PyObject* o, int64_t count, const Here& here, const char* what) {
+  if (o == Py_None) return nullptr;
+  const Tensor t(o, here);
+  want(t.is(std::is_same<T, float>::value ? kDLFloat : kDLInt, 32) && t.contiguous() && t.count() == count, what);
+  return static_cast<T*>(t.data());
+}
+// any tensor or None: its address, its bytes
+void* memory(PyObject* o, const Here& here, size_t* bytes = nullptr) {
+  if (o == Py_None) return nullptr;
+  const Tensor t(o, here);
+  if (bytes) *bytes = (size_t)t.count() * t.t.dtype.bits / 8;
+  return t.data();
 }
 struct Rows {  // [batch, rows, heads, dim], dim contiguous
   int64_t n[4], st[4];
-  PyObject* dtype;  // borrowed: torch's types live as long as torch
-  Rows(PyObject* t, const Here& here) {
-    here(t);
-    Ref d(PyObject_GetAttr(t, n_dtype));
-    dtype = d.p;
-    want(shape(t, n) == 4, "[sequences, rows, heads, head_dim] is wanted");
-    want(strides(t, st) == 4 && (n[3] == 1 || st[3] == 1), "head_dim must be contiguous");
+  void* data;
+  int32_t dtype;
+  Rows(PyObject* o, const Here& here) {
+    const Tensor t(o, here);
+    t.sizes(n, st, "[sequences, rows, heads, head_dim] is wanted");
+    want(n[3] == 1 || st[3] == 1, "head_dim must be contiguous");
+    data = t.data();
+    dtype = t.model_type(o);
   }
   void as(const Rows& o, bool heads_too) const {  // has the type and the sizes of others
     want(dtype == o.dtype, "types differ");
@@ -461,7 +511,7 @@ PyObject* append_paged(Args a) {
   const Here here;
   tsd_append_args t = {};
   const Rows k(a[1], here);
-  t.dtype = k.dtype == dtype_bf16 ? (int32_t)TSD_BF16 : dtype_code(a[1]);
+  t.dtype = k.dtype;
   k.to(t.kv_stride);
   t.batch = small(k.n[0]);
   t.n_rows = a[12] == Py_None ? small(k.n[1]) : to_i32(a[12]);
@@ -470,12 +520,12 @@ PyObject* append_paged(Args a) {
   if (t.n_blocks == 0) { t.n_blocks = 1; t.n_rows = 0; }
   t.n_kv_heads = small(k.n[2]);
   t.head_dim = small(k.n[3]);
-  t.k = ptr(a[1]);
+  t.k = k.data;
   if (a[2] != Py_None) {
     const Rows v(a[2], here);
     v.as(k, true);
     v.along(k);
-    t.v = ptr(a[2]);
+    t.v = v.data;
   }
   if (a[8] != Py_None) {
     want(a[9] != Py_None, "q wants a q_out");
@@ -485,8 +535,8 @@ PyObject* append_paged(Args a) {
     t.n_q_heads = small(q.n[2]);
     q.to(t.q_stride);
     o.to(t.q_out_stride);
-    t.q = ptr(a[8]);
-    t.q_out = ptr(a[9]);
+    t.q = q.data;
+    t.q_out = o.data;
   } else {
     want(a[9] == Py_None, "q_out wants a q");
   }
@@ -494,43 +544,44 @@ PyObject* append_paged(Args a) {
     const Rows o(a[10], here);
     o.as(k, true);
     o.to(t.k_out_stride);
-    t.k_out = ptr(a[10]);
+    t.k_out = o.data;
   }
-  t.first_slot = vec<int32_t>(a[3], dtype_i32, t.batch, here, "first_slot is a contiguous int32 [sequences]");
-  t.n_new = vec<int32_t>(a[4], dtype_i32, t.batch, here, "n_new is a contiguous int32 [sequences]");
-  t.positions = vec<int32_t>(a[5], dtype_i32, (int64_t)t.batch * t.n_rows, here, "positions is a contiguous int32 [sequences, n_rows]");
-  t.block = vec<int32_t>(a[11], dtype_i32, t.batch, here, "block is a contiguous int32 [sequences]");
+  t.first_slot = vec<int32_t>(a[3], t.batch, here, "first_slot is a contiguous int32 [sequences]");
+  t.n_new = vec<int32_t>(a[4], t.batch, here, "n_new is a contiguous int32 [sequences]");
+  t.positions = vec<int32_t>(a[5], (int64_t)t.batch * t.n_rows, here, "positions is a contiguous int32 [sequences, n_rows]");
+  t.block = vec<int32_t>(a[11], t.batch, here, "block is a contiguous int32 [sequences]");
   if (a[6] != Py_None) {
-    t.rotary_dim = small((int64_t)nbytes(a[6]) / 2);  // 4 bytes for every two dimensions
-    t.inv_freq = vec<float>(a[6], dtype_f32, t.rotary_dim / 2, here, "inv_freq is a contiguous fp32 [rotary_dim / 2]");
+    const int64_t pairs = Tensor(a[6], here).count();
+    t.rotary_dim = small(2 * pairs);
+    t.inv_freq = vec<float>(a[6], pairs, here, "inv_freq is a contiguous fp32 [rotary_dim / 2]");
   }
   t.interleaved = PyObject_IsTrue(a[7]);
-  here(a[13]);
-  t.status = ptr<uint32_t>(a[13]);
-  if (a[0] == Py_None) return done(call(tsd_append_paged_kv, &t, stream_of(a[14])), "tsd_append_paged_kv");
+  t.status = static_cast<uint32_t*>(memory(a[13], here));
+  if (a[0] == Py_None) return done(call(tsd_append_paged_kv, &t, here.stream(a[14])), "tsd_append_paged_kv");
   const Pages cache(a[0], here);
   t.cache = cache.get();
-  return done(call(tsd_append_paged_kv, &t, stream_of(a[14])), "tsd_append_paged_kv");
+  return done(call(tsd_append_paged_kv, &t, here.stream(a[14])), "tsd_append_paged_kv");
 }
 
 // cache, q, kv_lens, out, lse, sm_scale, workspace, status, stream
 PyObject* paged_attention(Args a) {
   const Here here;
   const Pages cache(a[0], here);
-  int64_t q[4], o[4], qs[4], os[4];
-  here(a[1]);
-  here(a[3]);
-  want(shape(a[1], q) == 3 && shape(a[3], o) == 3 && q[0] == o[0] && q[1] == o[1] && q[2] == o[2], "q and out are [sequences, heads, head_dim]");
-  want(strides(a[1], qs) == 3 && strides(a[3], os) == 3 && qs[2] == 1 && os[2] == 1, "head_dim must be contiguous");
+  const Tensor tq(a[1], here), to(a[3], here);
+  int64_t q[3], o[3], qs[3], os[3];
+  tq.sizes(q, qs, "q and out are [sequences, heads, head_dim]");
+  to.sizes(o, os, "q and out are [sequences, heads, head_dim]");
+  want(q[0] == o[0] && q[1] == o[1] && q[2] == o[2], "q and out are [sequences, heads, head_dim]");
+  want(qs[2] == 1 && os[2] == 1, "head_dim must be contiguous");
   want(q[0] == cache.get()->batch && q[2] == cache.get()->head_dim, "q has the cache's sequences and head_dim");
-  const int32_t dtype = dtype_code(a[1]);
-  want(dtype_code(a[3]) == dtype, "types of q and out differ");
-  here(a[6]);
-  here(a[7]);
-  return done(call(tsd_paged_attention, cache.get(), small(q[1]), dtype, ptr(a[1]), qs[0], qs[1],
-                   vec<int32_t>(a[2], dtype_i32, q[0], here, "kv_lens is a contiguous int32 [sequences]"), ptr(a[3]), os[0], os[1],
-                   vec<float>(a[4], dtype_f32, q[0] * q[1], here, "lse is a contiguous fp32 [sequences, heads]"), to_float(a[5]), ptr(a[6]),
-                   nbytes(a[6]), ptr<uint32_t>(a[7]), stream_of(a[8])),
+  const int32_t dtype = tq.model_type(a[1]);
+  want(to.model_type(a[3]) == dtype, "types of q and out differ");
+  size_t bytes = 0;
+  void* const workspace = memory(a[6], here, &bytes);
+  return done(call(tsd_paged_attention, cache.get(), small(q[1]), dtype, tq.data(), qs[0], qs[1],
+                   vec<int32_t>(a[2], q[0], here, "kv_lens is a contiguous int32 [sequences]"), to.data(), os[0], os[1],
+                   vec<float>(a[4], q[0] * q[1], here, "lse is a contiguous fp32 [sequences, heads]"), to_float(a[5]), workspace, bytes,
+                   static_cast<uint32_t*>(memory(a[7], here)), here.stream(a[8])),
               "tsd_paged_attention");
 }
 
@@ -544,18 +595,18 @@ PyObject* verify_attention_paged(Args a) {
   want(q.n[0] == l->batch && q.n[1] == (int64_t)l->n_branches * l->rows_per_branch && q.n[2] == l->n_q_heads && q.n[3] == l->head_dim,
        "q is [batch, branches * rows, n_q_heads, head_dim] of the layout");
   k.as(q, false);
-  want(k.n[2] == l->n_kv_heads && dtype_code(a[2]) == l->dtype, "draft rows have the layout's heads and type");
+  want(k.n[2] == l->n_kv_heads && q.dtype == l->dtype, "draft rows have the layout's heads and type");
   v.as(k, true);
   v.along(k);
   o.as(q, true);
-  here(a[1]);
-  here(a[9]);
-  here(a[11]);
-  want(a[1] != Py_None && nbytes(a[1]) >= tsd_branch_mask_bytes(l), "the mask is that of the layout");
-  return done(call(tsd_verify_attention_paged, l, ptr(a[1]), ptr(a[2]), q.st[0], q.st[1], q.st[2], cache.get(), ptr(a[4]), ptr(a[5]),
-                   k.st[0], k.st[1], k.st[2], ptr(a[6]), o.st[0], o.st[1], o.st[2],
-                   vec<float>(a[7], dtype_f32, q.n[0] * q.n[1] * q.n[2], here, "lse is a contiguous fp32 [batch, heads, rows]"),
-                   to_float(a[8]), ptr(a[9]), nbytes(a[9]), (uint32_t)to_int(a[10]), ptr<uint32_t>(a[11]), stream_of(a[12])),
+  size_t mask_bytes = 0, bytes = 0;
+  const void* const mask = memory(a[1], here, &mask_bytes);
+  void* const workspace = memory(a[9], here, &bytes);
+  want(mask && mask_bytes >= tsd_branch_mask_bytes(l), "the mask is that of the layout");
+  return done(call(tsd_verify_attention_paged, l, mask, q.data, q.st[0], q.st[1], q.st[2], cache.get(), k.data, v.data, k.st[0], k.st[1],
+                   k.st[2], o.data, o.st[0], o.st[1], o.st[2],
+                   vec<float>(a[7], q.n[0] * q.n[1] * q.n[2], here, "lse is a contiguous fp32 [batch, heads, rows]"), to_float(a[8]), workspace,
+                   bytes, (uint32_t)to_int(a[10]), static_cast<uint32_t*>(memory(a[11], here)), here.stream(a[12])),
               "tsd_verify_attention_paged");
 }
 
@@ -594,7 +645,7 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 #define TSD_METHOD(f, n) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<f, n>)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {TSD_METHOD(setup, 6),           TSD_METHOD(verify_attention, 14), TSD_METHOD(verify_attention_fp8, 16),
+PyMethodDef methods[] = {TSD_METHOD(setup, 7),           TSD_METHOD(verify_attention, 14), TSD_METHOD(verify_attention_fp8, 16),
                          TSD_METHOD(confidence_topk, 9), TSD_METHOD(accept, 19),           TSD_METHOD(accept_relaxed, 22),
                          TSD_METHOD(commit, 15),         TSD_METHOD(build_tree, 18),       TSD_METHOD(build_mask, 6),
                          TSD_METHOD(verify_step, 34),    TSD_METHOD(interblock_vis, 3),    TSD_METHOD(interblock_trigger, 10),
@@ -614,7 +665,6 @@ PyMODINIT_FUNC PyInit__tsd_native(void) {
   n_dtype = PyUnicode_InternFromString("dtype");
   n_cuda_stream = PyUnicode_InternFromString("cuda_stream");
   n_is_contiguous = PyUnicode_InternFromString("is_contiguous");
-  n_get_device = PyUnicode_InternFromString("get_device");
   n_device = PyUnicode_InternFromString("device");
   return PyModule_Create(&module);
 }
