@@ -389,7 +389,7 @@ __device__ __noinline__ void join_parts(const TokenParams& p, uint8_t* dynamic, 
 }
 
 template <int D, int kType, int HT>
-__global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) paged_attention_kernel(const __grid_constant__ TokenParams p) {
+__global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) token_attention_kernel(const __grid_constant__ TokenParams p) {
   using P = TokenPlan<D, kType, HT>;
   constexpr int NW = P::kWarps, KC = P::kKeys, NG = P::kGroups, NP = P::kPieces, NT = HT / 8;
   constexpr bool kF32 = kType == kTypeF32, kF16 = kType == kTypeE4m3;  // e4m3 is a subset of f16
@@ -1066,7 +1066,7 @@ static cudaError_t allow_smem() {
   if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
   std::lock_guard<std::mutex> lock(mu);
   if (done[dev]) return cudaSuccess;
-  e = cudaFuncSetAttribute(paged_attention_kernel<D, kType, HT>, cudaFuncAttributeMaxDynamicSharedMemorySize, TokenPlan<D, kType, HT>::kBytes);
+  e = cudaFuncSetAttribute(token_attention_kernel<D, kType, HT>, cudaFuncAttributeMaxDynamicSharedMemorySize, TokenPlan<D, kType, HT>::kBytes);
   done[dev] = e == cudaSuccess;
   return e;
 }
@@ -1080,9 +1080,9 @@ static int launch_token(const TokenParams& p, cudaStream_t stream) {
   const int64_t items = (int64_t)p.S * p.Hkv * p.tiles, per_item = (p.cache.cap + P::kKeys - 1) / P::kKeys;
   const int64_t grid = std::min<int64_t>(kTokenBlocks, p.S <= 32 ? items * ((per_item + P::kWarps - 1) / P::kWarps) : (most + P::kWarps - 1) / P::kWarps);
   cudaError_t e = allow_smem<D, kType, HT>();
-  if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(paged_attention_kernel)");
-  e = launch(paged_attention_kernel<D, kType, HT>, dim3((unsigned)std::max<int64_t>(grid, 1)), dim3(P::kWarps * 32), P::kBytes, stream, p);
-  return e != cudaSuccess ? cuda_fail(e, "paged_attention_kernel") : TSD_OK;
+  if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(token_attention_kernel)");
+  e = launch(token_attention_kernel<D, kType, HT>, dim3((unsigned)std::max<int64_t>(grid, 1)), dim3(P::kWarps * 32), P::kBytes, stream, p);
+  return e != cudaSuccess ? cuda_fail(e, "token_attention_kernel") : TSD_OK;
 }
 
 template <int D>
