@@ -625,7 +625,7 @@ int tsd_wait_block(int32_t batch, const uint64_t* report, uint32_t ticket, int32
  *   page_table   device int32 [batch, max_pages], sequences table_stride entries apart.  Only the entries of
  *                tokens that a call reads or writes are looked at.  One of those outside [0, n_pages) sets
  *                TSD_STATUS_BAD_INDEX: its tokens are not written, and read as rows of zeros.
- *   page_size    8, 16, 32, ... 1024;  max_pages * page_size at most 2^31 - 1024.
+ *   page_size    8, 16, 32, ... 1024;  max_pages * page_size at most 2^31 - 4096.
  *   head_dim     64 or 128;  dtype TSD_F32, TSD_BF16 or TSD_E4M3 (with queries, new rows and outputs in bf16).
  * Pages may be shared by sequences that only read them.
  * ------------------------------------------------------------------------- */

@@ -22,8 +22,8 @@ int check_paged_cache(const tsd_paged_cache* c) {
   if (c->batch < 1 || c->n_pages < 1 || c->max_pages < 1 || c->n_kv_heads < 1 || c->table_stride < 0) return TSD_ERR_INVALID_ARG;
   if (c->page_size < 1) return TSD_ERR_INVALID_ARG;
   if (c->page_size < 8 || c->page_size > 1024 || (c->page_size & (c->page_size - 1))) return TSD_ERR_UNSUPPORTED;
-  // room behind the last token for the kernels to count on to the end of a tile
-  if ((int64_t)c->max_pages * c->page_size > 0x80000000ll - 1024) return TSD_ERR_INVALID_ARG;
+  // room behind the last token for the kernels to count on: 32 tiles of 64 keys in the verification pass, whose lanes look up a tile's page each
+  if ((int64_t)c->max_pages * c->page_size > 0x80000000ll - 4096) return TSD_ERR_INVALID_ARG;
   if (c->batch > 1 && c->table_stride < c->max_pages) return TSD_ERR_INVALID_ARG;
   if (c->head_dim != 64 && c->head_dim != 128) return TSD_ERR_UNSUPPORTED;
   if (c->dtype != TSD_F32 && c->dtype != TSD_BF16 && c->dtype != TSD_E4M3) return TSD_ERR_UNSUPPORTED;

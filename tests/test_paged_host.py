@@ -158,7 +158,7 @@ def test_results_that_would_meet_and_sizes_at_the_limit(lib):
     for kw in (dict(q_out_stride=(0, 3584, 128)), dict(q_out_stride=(96 * 3584, 0, 128)), dict(k_out=P, k_out_stride=(96 * 512, 0, 128))):
         assert append(lib, **kw) == bad, kw
     need = lambda **kw: lib.tsd_paged_attention_workspace_bytes(ctypes.byref(cache(**kw)), 28)
-    assert need(page_size=1024, max_pages=(1 << 21) - 1, table_stride=1 << 21) > 0
-    assert need(page_size=1024, max_pages=1 << 21, table_stride=1 << 21) == 0
-    assert need(page_size=8, max_pages=(1 << 28) - 128, table_stride=1 << 28) > 0
-    assert need(page_size=8, max_pages=(1 << 28) - 127, table_stride=1 << 28) == 0
+    assert need(page_size=1024, max_pages=(1 << 21) - 4, table_stride=1 << 21) > 0
+    assert need(page_size=1024, max_pages=(1 << 21) - 3, table_stride=1 << 21) == 0
+    assert need(page_size=8, max_pages=(1 << 28) - 512, table_stride=1 << 28) > 0
+    assert need(page_size=8, max_pages=(1 << 28) - 511, table_stride=1 << 28) == 0
