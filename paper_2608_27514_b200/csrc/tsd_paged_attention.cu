@@ -5,7 +5,7 @@
 // serves to keep loads in flight and the work behind them short.
 //   split   : the keys of all sequences and heads are laid end to end in chunks of 4 KB of K and 4 KB of V (16 keys of 128 bf16) and cut over
 //             the blocks, one per SM, evenly or item by item (an item: a sequence and a tile of the heads that share one of its kv
-//             heads).  A block's warps take an even stretch of its chunks each, and walk it without waiting for one another.
+//             heads), by the device from the lengths, or, where the caches are short, by the host: a cluster of blocks for every item.  A block's warps take an even stretch of its chunks each, and walk it without waiting for one another.
 //   queue   : every warp has its next chunk on the way to shared memory while it works on one (cp.async): 12 warps, 96 KB per SM.  (16 warps
 //             with fewer registers: spills; 2 blocks of 8 warps: slower by 3-5 %, another round of joins.)
 //   products: mma.sync m16n8k16 with K (16 keys) or V^T (16 dimensions) as the 16 rows and the heads as the 8 columns: no part of a product is
@@ -19,12 +19,13 @@
 //   fp32    : the same queue on CUDA cores (the scores' partial sums of a key meet over its 4 lanes, the weights in shared memory).
 //   join    : an item that a warp has from its first chunk to its last is written out at once.  Otherwise the warps' offsets, sums and rows meet
 //             in shared memory, and what is not the whole of its item goes to the workspace: the last of the item's blocks to
-//             arrive puts the parts together, in their order whoever arrives last, so that results repeat bit by bit.
+//             arrive puts the parts together, in their order whoever arrives last, so that results repeat bit by bit.  The blocks
+//             of a cluster read one another's parts in shared memory instead.
 // Lengths are read on the device: a captured call follows them.  Rows past a length are not loaded.
 // Measured (caches larger than L2): 2 sequences of 131072 rows, 28/4 heads of 128, bf16, pages of 64: 85.7 us, 6.27 TB/s, 95 % of what a copy
 // reaches; the same in e4m3: 50.3 us, 5.3 TB/s, where conversions come beside the loads; 48 ragged sequences of up to 4096: 39.9 us, 4.8
 // TB/s.  A call costs about 6 us before its bytes count (the launch and two dependent reads, 2 us; the first chunk on its way, 1 us; the
-// warps' parts, 1 us; the blocks', 2 us): 1 sequence of 768 rows, 32 heads (12.6 MB): 8.9 us.
+// warps' parts, 1 us; the blocks', 2 us), with clusters 4: 1 sequence of 768 rows, 32 heads (12.6 MB): 6.5 us.
 #include <cuda_fp16.h>
 #include <algorithm>
 #include <cfloat>
@@ -56,6 +57,8 @@ struct TokenPlan {
   static constexpr int kQueue = kWarps * 8192;
   static constexpr int kPart = HT * D;                                         // floats: at most a warp's queue
   static constexpr int kBytes = kQueue + kWarps * kPart * 4;
+  template <bool kItems>
+  static constexpr int kBytesFor = kBytes + (kItems ? kSlot * 4 : 0);          // and the block's part, for the others of its cluster
 };
 
 struct TokenParams {
@@ -66,6 +69,7 @@ struct TokenParams {
   const int32_t* lens;
   int64_t q_b, q_h, o_b, o_h;
   int S, Hq, Hkv, group, tiles;  // tiles: of HT heads per kv head
+  int shift;                     // 2^shift blocks per item, where the host cuts
   float scale_log2e;
   float* parts;        // [2 * blocks] slots: a block's part of the item that began in a block before it (even), of one that goes on behind it (odd)
   unsigned* tickets;   // per block in which a shared sequence begins
@@ -144,7 +148,7 @@ template <int D, int kType, int HT>
 struct TokenShared {
   static constexpr int NW = TokenPlan<D, kType, HT>::kWarps;
   float part_m[2 * NW][HT], part_l[2 * NW][HT];
-  Item part_item[2 * NW];  // whose (n = 0: no part)
+  Item part_item[2 * NW + 1];  // whose (n = 0: no part); the last: the block's one item, where the host cuts
   int part_first[2 * NW];  // its first chunk
   int last_arrival[2];
   int x0, x1, each, more;     // the block's share; how the blocks' shares are cut
@@ -192,12 +196,133 @@ __device__ __forceinline__ Item item_after(const TokenParams& p, Item i) {
   return i;
 }
 
+// Row `row` of the block's parts in `of`, by one warp: offset, sum and 4 dimensions per lane.
+template <int D, int kType, int HT>
+__device__ __forceinline__ void parts_together(TokenShared<D, kType, HT>& sh, uint8_t* dynamic, unsigned of, int row, float& top, float& sum, float4& o) {
+  constexpr unsigned full = 0xffffffffu;
+  const int lane = threadIdx.x & 31;
+  const bool in = (of >> lane) & 1;
+  const float mine = in ? sh.part_m[lane][row] : -CUDART_INF_F;
+  top = mine;
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(full, top, off));
+  const float weight = in ? exp2_approx(mine - top) : 0.f;
+  sum = in ? sh.part_l[lane][row] * weight : 0.f;
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(full, sum, off);
+  o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+  while (of) {  // four at a time
+    float4 v[4];
+    float f[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = of ? __ffs(of) - 1 : 0;
+      f[k] = __shfl_sync(full, weight, i);
+      if (!of) f[k] = 0.f;
+      v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (of) v[k] = *reinterpret_cast<const float4*>(part_of<D, kType, HT>(dynamic, i) + row * D + 4 * (D == 128 ? lane : lane & 15));
+      of &= of - 1;  // 0 stays 0
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      o.x = fmaf(v[k].x, f[k], o.x); o.y = fmaf(v[k].y, f[k], o.y); o.z = fmaf(v[k].z, f[k], o.z); o.w = fmaf(v[k].w, f[k], o.w);
+    }
+  }
+}
+// A row's result.
+template <int D, int kType>
+__device__ __forceinline__ void write_row_of(const TokenParams& p, const Item& item, int row, float top, float sum, const float4& o) {
+  constexpr bool kF32 = kType == kTypeF32, kF16 = kType == kTypeE4m3;
+  const int lane = threadIdx.x & 31;
+  const float v_scale = kF16 && p.cache.v_scale ? p.cache.v_scale[item.kv] : 1.f, f = kF32 ? v_scale / sum : __fdividef(v_scale, sum);
+  const int head = item.h0 + row;
+  const int64_t to = item.s * p.o_b + (int64_t)head * p.o_h + 4 * lane;
+  if (D == 128 || lane < 16) {
+    if constexpr (kF32) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to) = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+    else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + to) = make_uint2(bf16_pair(o.x * f, o.y * f), bf16_pair(o.z * f, o.w * f));
+  }
+  if (p.lse && lane == 0) p.lse[(int64_t)item.s * p.Hq + head] = (top + log2f(sum)) * kLn2;
+}
+
+__device__ __forceinline__ uint32_t at_rank(const void* p, int rank) {  // the same place in another block of the cluster
+  uint32_t a;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ float peer_float(const float* p, int rank) {
+  float x;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at_rank(p, rank)) : "memory");
+  return x;
+}
+__device__ __forceinline__ float4 peer_float4(const float* p, int rank) {
+  float4 x;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(at_rank(p, rank)) : "memory");
+  return x;
+}
+// What follows the loop where an item has 2^shift blocks of its own, a cluster: the warps' parts meet in the block's shared memory, the
+// blocks' are read from one another's.  (Joining 4 blocks
+// through the workspace, with the cut on the device, takes 2.3 us more: 1 sequence of 768 rows, 32 heads 8.8 us, 6.5 so.)
+template <int D, int kType, int HT>
+__device__ __noinline__ void join_cluster(const TokenParams& p, uint8_t* dynamic, TokenShared<D, kType, HT>& sh) {
+  using P = TokenPlan<D, kType, HT>;
+  constexpr int NW = P::kWarps;
+  constexpr unsigned full = 0xffffffffu;
+  const int warp = __shfl_sync(full, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, blocks = 1 << p.shift;
+  float* const slot = reinterpret_cast<float*>(dynamic + P::kBytes);
+  __syncthreads();
+  const unsigned of = __ballot_sync(full, lane < 2 * NW && sh.part_item[lane].n > 0);  // all of the one item
+  const Item it = sh.part_item[2 * NW];
+#pragma unroll 1
+  for (int row = warp; row < it.rows; row += NW) {
+    float top = -CUDART_INF_F, sum = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (of) {
+      parts_together<D, kType, HT>(sh, dynamic, of, row, top, sum, o);
+      if (blocks == 1) write_row_of<D, kType>(p, it, row, top, sum, o);
+    }
+    if (D == 128 || lane < 16) *reinterpret_cast<float4*>(slot + row * D + 4 * lane) = o;
+    if (lane == 0) { slot[HT * D + row] = top; slot[HT * D + HT + row] = sum; }
+  }
+  if (blocks == 1) return;
+  asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+  const int rank = (int)blockIdx.x & (blocks - 1);
+#pragma unroll 1
+  for (int row = rank + (warp << p.shift); row < it.rows; row += NW << p.shift) {
+    const bool in = lane < blocks;
+    const float mine = in ? peer_float(slot + HT * D + row, lane) : -CUDART_INF_F, sum_mine = in ? peer_float(slot + HT * D + HT + row, lane) : 0.f;
+    float4 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i < blocks) v[i] = peer_float4(slot + row * D + 4 * (D == 128 ? lane : lane & 15), i);
+    }
+    float top = mine;
+#pragma unroll
+    for (int off = 4; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(full, top, off));
+    top = __shfl_sync(full, top, 0);
+    if (top == -CUDART_INF_F) continue;  // no block had a part: no keys, or one chunk, which its warp has written
+    const float weight = in ? exp2_approx(mine - top) : 0.f;
+    float sum = sum_mine * weight;
+#pragma unroll
+    for (int off = 4; off >= 1; off >>= 1) sum += __shfl_xor_sync(full, sum, off);
+    sum = __shfl_sync(full, sum, 0);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float f = __shfl_sync(full, weight, i);
+      o.x = fmaf(v[i].x, f, o.x); o.y = fmaf(v[i].y, f, o.y); o.z = fmaf(v[i].z, f, o.z); o.w = fmaf(v[i].w, f, o.w);
+    }
+    write_row_of<D, kType>(p, it, row, top, sum, o);
+  }
+  asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");  // no block leaves before its parts are read
+}
+
 // What follows the loop over the chunks, a function of its own so that it takes no registers from that loop.
 template <int D, int kType, int HT>
 __device__ __noinline__ void join_parts(const TokenParams& p, uint8_t* dynamic, TokenShared<D, kType, HT>& sh) {
   using P = TokenPlan<D, kType, HT>;
   constexpr int NW = P::kWarps;
-  constexpr bool kF32 = kType == kTypeF32, kF16 = kType == kTypeE4m3;
   constexpr unsigned full = 0xffffffffu;
   // the shuffle tells the compiler that the warp branches together, a third of this function's code
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, x0 = sh.x0, x1 = sh.x1, each = sh.each, more = sh.more;
@@ -216,47 +341,8 @@ __device__ __noinline__ void join_parts(const TokenParams& p, uint8_t* dynamic, 
     count = sh.item_blocks ? sh.item_blocks : block_of(first + n - 1) - b_first + 1;
   };
   // ---- the block's parts: put together where they are of one sequence, then written out, or, where other blocks have the rest, to the workspace
-  // Row `row` of the parts in `of`, by one warp: offset, sum and 4 dimensions per lane.
-  auto together = [&](unsigned of, int row, float& top, float& sum, float4& o) {
-    const bool in = (of >> lane) & 1;
-    const float mine = in ? part_m[lane][row] : -CUDART_INF_F;
-    top = mine;
-#pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(full, top, off));
-    const float weight = in ? exp2_approx(mine - top) : 0.f;
-    sum = in ? part_l[lane][row] * weight : 0.f;
-#pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(full, sum, off);
-    o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-    while (of) {  // four at a time
-      float4 v[4];
-      float f[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int i = of ? __ffs(of) - 1 : 0;
-        f[k] = __shfl_sync(full, weight, i);
-        if (!of) f[k] = 0.f;
-        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (of) v[k] = *reinterpret_cast<const float4*>(part_of(i) + row * D + 4 * (D == 128 ? lane : lane & 15));
-        of &= of - 1;  // 0 stays 0
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        o.x = fmaf(v[k].x, f[k], o.x); o.y = fmaf(v[k].y, f[k], o.y); o.z = fmaf(v[k].z, f[k], o.z); o.w = fmaf(v[k].w, f[k], o.w);
-      }
-    }
-  };
-  auto write_row = [&](const Item& item, int row, float top, float sum, const float4& o) {
-    const float v_scale = kF16 && p.cache.v_scale ? p.cache.v_scale[item.kv] : 1.f, f = kF32 ? v_scale / sum : __fdividef(v_scale, sum);
-    const int head = item.h0 + row;
-    const int64_t to = item.s * p.o_b + (int64_t)head * p.o_h + 4 * lane;
-    if (D == 128 || lane < 16) {
-      if constexpr (kF32) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to) = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
-      else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + to) = make_uint2(bf16_pair(o.x * f, o.y * f), bf16_pair(o.z * f, o.w * f));
-    }
-    if (p.lse && lane == 0) p.lse[(int64_t)item.s * p.Hq + head] = (top + log2f(sum)) * kLn2;
-  };
+  auto together = [&](unsigned of, int row, float& top, float& sum, float4& o) { parts_together<D, kType, HT>(sh, dynamic, of, row, top, sum, o); };
+  auto write_row = [&](const Item& item, int row, float top, float sum, const float4& o) { write_row_of<D, kType>(p, item, row, top, sum, o); };
   __syncthreads();
   int shared0 = 0, shared1 = 0, n_shared = 0;  // parts with which items of several blocks begin in this one: at most two
   {
@@ -388,7 +474,8 @@ __device__ __noinline__ void join_parts(const TokenParams& p, uint8_t* dynamic, 
   }
 }
 
-template <int D, int kType, int HT>
+// kItems: the host has cut, 2^shift blocks for every item, a cluster of them
+template <int D, int kType, int HT, bool kItems>
 __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) token_attention_kernel(const __grid_constant__ TokenParams p) {
   using P = TokenPlan<D, kType, HT>;
   constexpr int NW = P::kWarps, KC = P::kKeys, NG = P::kGroups, NP = P::kPieces, NT = HT / 8;
@@ -408,99 +495,117 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) token
   auto length = [&](int s) { return length_of(a, s); };
   auto chunks = [&](int len) { return (int)(((unsigned)len + KC - 1) / KC); };
 
-  // ---- this block's share [x0, x1) of all chunks (fewer than 2^30: checked on the host)
-  // Up to 32 sequences: a lane each, every warp for itself.  More: a thread for a run of them, whose chunks are added up over the block.
-  int total;
-  const int len0 = lane < a.S ? length(lane) : 0;  // of the first 32 sequences
-  const int run = a.S <= 32 ? 0 : (int)((unsigned)(a.S + NW * 32 - 1) / (NW * 32));
-  if (run == 0) {
-    total = __reduce_add_sync(full, chunks(len0));
+  int x0, x1, total = 0, run = 0, len0 = 0;  // this block's share [x0, x1) of the chunks, of an item or of all
+  Item next;       // the item whose chunk is fetched next, unless the one at hand goes on,
+  int next_c = 0;  // and that chunk
+  if constexpr (kItems) {
+    const int item = (int)(blockIdx.x >> a.shift), in_item = (int)blockIdx.x & ((1 << a.shift) - 1);
+    next.s = (int)((unsigned)item / (unsigned)HI);
+    const int hi = item - next.s * HI;
+    next.kv = a.tiles == 1 ? hi : (int)((unsigned)hi / (unsigned)a.tiles);
+    const int tile = hi - next.kv * a.tiles;
+    next.h0 = next.kv * a.group + tile * HT;
+    next.rows = min(HT, a.group - tile * HT);
+    next.len = length(next.s);
+    next.n = chunks(next.len);
+    const int even = next.n >> a.shift, rest = next.n & ((1 << a.shift) - 1);
+    x0 = in_item * even + min(in_item, rest);
+    x1 = x0 + even + (in_item < rest ? 1 : 0);
+    if (tid == 0) shared.part_item[2 * NW] = next;
   } else {
-    int mine = 0;
+    // ---- this block's share [x0, x1) of all chunks (fewer than 2^30: checked on the host)
+    // Up to 32 sequences: a lane each, every warp for itself.  More: a thread for a run of them, whose chunks are added up over the block.
+    len0 = lane < a.S ? length(lane) : 0;  // of the first 32 sequences
+    run = a.S <= 32 ? 0 : (int)((unsigned)(a.S + NW * 32 - 1) / (NW * 32));
+    if (run == 0) {
+      total = __reduce_add_sync(full, chunks(len0));
+    } else {
+      int mine = 0;
 #pragma unroll 4
-    for (int k = 0; k < run; ++k) mine += tid * run + k < a.S ? chunks(length(tid * run + k)) : 0;
-    int upto = mine;
+      for (int k = 0; k < run; ++k) mine += tid * run + k < a.S ? chunks(length(tid * run + k)) : 0;
+      int upto = mine;
 #pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int o = __shfl_up_sync(full, upto, off);
-      if (lane >= off) upto += o;
-    }
-    if (lane == 31) shared.warp_chunks[warp] = upto;
-    __syncthreads();
-    const int of_warp = lane < NW ? shared.warp_chunks[lane] : 0;
-    total = __reduce_add_sync(full, of_warp);
-    shared.run_first[tid] = upto - mine + __reduce_add_sync(full, lane < warp ? of_warp : 0);
-    __syncthreads();
-  }
-  total *= HI;
-  // The chunks of up to 32 sequences are cut item by item, into equal pieces, one per block: then a block has parts of one item only and one
-  // arrival to wait for, and fewer blocks than SMs have the memory's rate too.  That is worth pieces a quarter longer than an
-  // even share.  Where there is little to do a piece is a chunk for each of the block's warps, and two if that leaves no item to
-  // more than one block.  Otherwise, and for more sequences, the blocks take `each` chunks, the first `more` of them one more, wherever
-  // that cuts the items.  (16 sequences of 2048, 8 kv heads, in 128 blocks instead of 148: 27.4 us instead of 30.8; 120 heads of one sequence
-  // of 8192 in 120: 78.2, 82.5; with pieces a half longer 50 heads in 100 blocks 73.6, 72.1, in e4m3 50.4, 44.0.  8 items of 16 chunks, in
-  // 8 blocks instead of 11: 7.5 us instead of 10.2; 32 items of 8 chunks, in 32 blocks instead of 22: 6.5 instead of 11.1.  A third chunk
-  // per warp is not worth it: 36 chunks 9.5 us in one block, 8.9 in three.)
-  const int n0 = chunks(len0), longest = __reduce_max_sync(full, n0);
-  const int for_warps = a.S <= 32 ? HI * __reduce_add_sync(full, (n0 + NW - 1) / NW) : (total + NW - 1) / NW;
-  const int most_blocks = max(1, min((int)gridDim.x, for_warps));
-  const int each = (int)((unsigned)total / (unsigned)most_blocks), more = total - each * most_blocks;
-  int x0, x1, item_blocks = 0, in_item = 0;  // of the block's item, if they are cut one by one: blocks, and which of them this is
-  int pieces = 0;                         // of each item of the lane's sequence
-  if (a.S <= 32 && total > 0) {
-    auto fit = [&](int piece) {  // a quotient that is off by a rounding is as good: what counts is the pieces' number
-      pieces = n0 > 0 ? max(1, (int)ceilf(__fdividef((float)n0, (float)piece))) : 0;
-      return HI * __reduce_add_sync(full, pieces) <= most_blocks;
-    };
-    int lo = each + (more > 0) - 1, hi = each + 2 + each / kAlignSlack;  // the smallest that fits is looked for in (lo, hi]
-    if (for_warps == most_blocks) { hi = NW; lo = hi - 1; }
-    if (longest <= 2 * NW && HI * __popc(__ballot_sync(full, n0 > 0)) <= most_blocks) { hi = longest; lo = hi - 1; }
-    if (fit(hi)) {
-      item_blocks = 1;
-      int best = pieces;
-#pragma unroll 1
-      for (int tries = 0; tries < 5 && lo + 1 < hi; ++tries) {
-        const int mid = (lo + hi) >> 1;
-        if (fit(mid)) { hi = mid; best = pieces; }
-        else lo = mid;
+      for (int off = 1; off < 32; off <<= 1) {
+        const int o = __shfl_up_sync(full, upto, off);
+        if (lane >= off) upto += o;
       }
-      pieces = best;
+      if (lane == 31) shared.warp_chunks[warp] = upto;
+      __syncthreads();
+      const int of_warp = lane < NW ? shared.warp_chunks[lane] : 0;
+      total = __reduce_add_sync(full, of_warp);
+      shared.run_first[tid] = upto - mine + __reduce_add_sync(full, lane < warp ? of_warp : 0);
+      __syncthreads();
     }
-  }
-  if (item_blocks) {
-    int blocks_upto = pieces * HI, chunks_upto = n0 * HI;
+    total *= HI;
+    // The chunks of up to 32 sequences are cut item by item, into equal pieces, one per block: then a block has parts of one item only and one
+    // arrival to wait for, and fewer blocks than SMs have the memory's rate too.  That is worth pieces a quarter longer than an
+    // even share.  Where there is little to do a piece is a chunk for each of the block's warps, and two if that leaves no item to
+    // more than one block.  Otherwise, and for more sequences, the blocks take `each` chunks, the first `more` of them one more, wherever
+    // that cuts the items.  (16 sequences of 2048, 8 kv heads, in 128 blocks instead of 148: 27.4 us instead of 30.8; 120 heads of one sequence
+    // of 8192 in 120: 78.2, 82.5; with pieces a half longer 50 heads in 100 blocks 73.6, 72.1, in e4m3 50.4, 44.0.  8 items of 16 chunks, in
+    // 8 blocks instead of 11: 7.5 us instead of 10.2; 32 items of 8 chunks, in 32 blocks instead of 22: 6.5 instead of 11.1.  A third chunk
+    // per warp is not worth it: 36 chunks 9.5 us in one block, 8.9 in three.)
+    const int n0 = chunks(len0), longest = __reduce_max_sync(full, n0);
+    const int for_warps = a.S <= 32 ? HI * __reduce_add_sync(full, (n0 + NW - 1) / NW) : (total + NW - 1) / NW;
+    const int most_blocks = max(1, min((int)gridDim.x, for_warps));
+    const int each = (int)((unsigned)total / (unsigned)most_blocks), more = total - each * most_blocks;
+    int item_blocks = 0, in_item = 0;  // of the block's item, if they are cut one by one: blocks, and which of them this is
+    int pieces = 0;                         // of each item of the lane's sequence
+    if (a.S <= 32 && total > 0) {
+      auto fit = [&](int piece) {  // a quotient that is off by a rounding is as good: what counts is the pieces' number
+        pieces = n0 > 0 ? max(1, (int)ceilf(__fdividef((float)n0, (float)piece))) : 0;
+        return HI * __reduce_add_sync(full, pieces) <= most_blocks;
+      };
+      int lo = each + (more > 0) - 1, hi = each + 2 + each / kAlignSlack;  // the smallest that fits is looked for in (lo, hi]
+      if (for_warps == most_blocks) { hi = NW; lo = hi - 1; }
+      if (longest <= 2 * NW && HI * __popc(__ballot_sync(full, n0 > 0)) <= most_blocks) { hi = longest; lo = hi - 1; }
+      if (fit(hi)) {
+        item_blocks = 1;
+        int best = pieces;
+#pragma unroll 1
+        for (int tries = 0; tries < 5 && lo + 1 < hi; ++tries) {
+          const int mid = (lo + hi) >> 1;
+          if (fit(mid)) { hi = mid; best = pieces; }
+          else lo = mid;
+        }
+        pieces = best;
+      }
+    }
+    if (item_blocks) {
+      int blocks_upto = pieces * HI, chunks_upto = n0 * HI;
 #pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int o = __shfl_up_sync(full, blocks_upto, off), c = __shfl_up_sync(full, chunks_upto, off);
-      if (lane >= off) { blocks_upto += o; chunks_upto += c; }
+      for (int off = 1; off < 32; off <<= 1) {
+        const int o = __shfl_up_sync(full, blocks_upto, off), c = __shfl_up_sync(full, chunks_upto, off);
+        if (lane >= off) { blocks_upto += o; chunks_upto += c; }
+      }
+      const unsigned hit = __ballot_sync(full, blocks_upto > (int)blockIdx.x);
+      const int l = hit ? __ffs(hit) - 1 : 0;
+      item_blocks = __shfl_sync(full, pieces, l);
+      const int n = __shfl_sync(full, n0, l), b = (int)blockIdx.x - (__shfl_sync(full, blocks_upto, l) - item_blocks * HI);
+      const int hi = hit ? (int)((unsigned)b / (unsigned)item_blocks) : 0;
+      in_item = b - hi * item_blocks;
+      const int first = __shfl_sync(full, chunks_upto, l) - n * HI + hi * n;
+      const int even = hit ? (int)((unsigned)n / (unsigned)item_blocks) : 0, rest = n - even * item_blocks;
+      x0 = hit ? first + in_item * even + min(in_item, rest) : total;
+      x1 = hit ? x0 + even + (in_item < rest ? 1 : 0) : total;
+    } else {
+      const int b = min((int)blockIdx.x, most_blocks);
+      x0 = b * each + min(b, more);
+      x1 = b == most_blocks ? total : x0 + each + (b < more ? 1 : 0);
     }
-    const unsigned hit = __ballot_sync(full, blocks_upto > (int)blockIdx.x);
-    const int l = hit ? __ffs(hit) - 1 : 0;
-    item_blocks = __shfl_sync(full, pieces, l);
-    const int n = __shfl_sync(full, n0, l), b = (int)blockIdx.x - (__shfl_sync(full, blocks_upto, l) - item_blocks * HI);
-    const int hi = hit ? (int)((unsigned)b / (unsigned)item_blocks) : 0;
-    in_item = b - hi * item_blocks;
-    const int first = __shfl_sync(full, chunks_upto, l) - n * HI + hi * n;
-    const int even = hit ? (int)((unsigned)n / (unsigned)item_blocks) : 0, rest = n - even * item_blocks;
-    x0 = hit ? first + in_item * even + min(in_item, rest) : total;
-    x1 = hit ? x0 + even + (in_item < rest ? 1 : 0) : total;
-  } else {
-    const int b = min((int)blockIdx.x, most_blocks);
-    x0 = b * each + min(b, more);
-    x1 = b == most_blocks ? total : x0 + each + (b < more ? 1 : 0);
-  }
-  if (tid == 0) {
-    shared.x0 = x0; shared.x1 = x1; shared.each = each; shared.more = more;
-    shared.item_blocks = item_blocks; shared.in_item = in_item;
+    if (tid == 0) {
+      shared.x0 = x0; shared.x1 = x1; shared.each = each; shared.more = more;
+      shared.item_blocks = item_blocks; shared.in_item = in_item;
+    }
   }
   // and its warps an even share of that, [w0, w1) for this one
   const unsigned share = (unsigned)(x1 - x0) / NW, longer = (unsigned)(x1 - x0) % NW;
   const int w0 = x0 + (int)(warp * share + min((unsigned)warp, longer)), w1 = w0 + (int)(share + (warp < (int)longer ? 1 : 0));
 
   // ---- where chunk w0 lies
-  Item next;       // the item whose chunk is fetched next, unless the one at hand goes on,
-  int next_c = 0;  // and that chunk
-  {
+  if constexpr (kItems) {
+    next_c = w0;
+  } else {
     int before = 0;
     next.s = 0;
     next.len = 0;
@@ -1027,7 +1132,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) token
     fresh = ends;
     if (ends && more_chunks) {
       item = next;
-      if (x + 1 + item.n - c < w1) {  // the warp has chunks of another one behind it
+      if (!kItems && x + 1 + item.n - c < w1) {  // the warp has chunks of another one behind it
         next = item_after<KC, HT>(p, next);
         next_c = 0;
         next_entry = entry_of(next, 0);
@@ -1035,7 +1140,8 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) token
     }
   }
 
-  join_parts<D, kType, HT>(p, dynamic, shared);
+  if constexpr (kItems) join_cluster<D, kType, HT>(p, dynamic, shared);
+  else join_parts<D, kType, HT>(p, dynamic, shared);
 
   // sequences without keys
 #pragma unroll 1
@@ -1055,7 +1161,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) token
 static int head_tile(int group) { return group <= 8 ? 8 : 16; }
 
 // The kernel's dynamic shared memory limit, an attribute per device.
-template <int D, int kType, int HT>
+template <int D, int kType, int HT, bool kItems>
 static cudaError_t allow_smem() {
   constexpr int kMaxDevices = 64;
   static std::mutex mu;
@@ -1066,23 +1172,42 @@ static cudaError_t allow_smem() {
   if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
   std::lock_guard<std::mutex> lock(mu);
   if (done[dev]) return cudaSuccess;
-  e = cudaFuncSetAttribute(token_attention_kernel<D, kType, HT>, cudaFuncAttributeMaxDynamicSharedMemorySize, TokenPlan<D, kType, HT>::kBytes);
+  e = cudaFuncSetAttribute(token_attention_kernel<D, kType, HT, kItems>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           TokenPlan<D, kType, HT>::template kBytesFor<kItems>);
   done[dev] = e == cudaSuccess;
   return e;
 }
 
-template <int D, int kType, int HT>
-static int launch_token(const TokenParams& p, cudaStream_t stream) {
+template <int D, int kType, int HT, bool kItems>
+static int launch_token(const TokenParams& p, int64_t grid, cudaStream_t stream) {
   using P = TokenPlan<D, kType, HT>;
-  const int64_t most = (int64_t)p.S * p.Hkv * p.tiles * ((p.cache.cap + P::kKeys - 1) / P::kKeys);  // chunks, if every sequence were full
-  if (most >= (1 << 30)) return TSD_ERR_UNSUPPORTED;
-  // a chunk for each of a block's warps; up to 32 sequences may be cut item by item
-  const int64_t items = (int64_t)p.S * p.Hkv * p.tiles, per_item = (p.cache.cap + P::kKeys - 1) / P::kKeys;
-  const int64_t grid = std::min<int64_t>(kTokenBlocks, p.S <= 32 ? items * ((per_item + P::kWarps - 1) / P::kWarps) : (most + P::kWarps - 1) / P::kWarps);
-  cudaError_t e = allow_smem<D, kType, HT>();
+  cudaError_t e = allow_smem<D, kType, HT, kItems>();
   if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(token_attention_kernel)");
-  e = launch(token_attention_kernel<D, kType, HT>, dim3((unsigned)std::max<int64_t>(grid, 1)), dim3(P::kWarps * 32), P::kBytes, stream, p);
+  e = launch_clusters(1 << p.shift, token_attention_kernel<D, kType, HT, kItems>, dim3((unsigned)grid), dim3(P::kWarps * 32), P::template kBytesFor<kItems>,
+                      stream, p);
   return e != cudaSuccess ? cuda_fail(e, "token_attention_kernel") : TSD_OK;
+}
+
+template <int D, int kType, int HT>
+static int launch_token(TokenParams p, cudaStream_t stream) {
+  using P = TokenPlan<D, kType, HT>;
+  const int64_t items = (int64_t)p.S * p.Hkv * p.tiles, per_item = (p.cache.cap + P::kKeys - 1) / P::kKeys;
+  const int64_t most = items * per_item;  // chunks, if every sequence were full
+  if (most >= (1 << 30)) return TSD_ERR_UNSUPPORTED;
+  // Short caches: the host cuts, 1, 2, 4 or 8 blocks for every item, a cluster that joins in shared memory and needs to look at one length
+  // only.  One block where its warps have a chunk each, otherwise as many as there is room for (clusters of 4 find SMs for 128
+  // blocks, clusters of 8 for fewer than 128: 16 of them take 15.3 us where 16 items cut by the device take 11.3), as long as a warp
+  // gets no more than three chunks.  Clusters against the device's cut: 32 items of 48 chunks 6.5 us, 8.8; 8 of 16 5.6, 7.5 (in 2 blocks 6.2);
+  // 32 of 8, in a block each, 4.9, 6.3 (in 2 blocks 5.7); 8 of 256 9.4, 11.0; 8 of 375 (four chunks) 11.1, 11.4, and 4 of 375
+  // 11.3, 11.0.  Where lengths are ragged and three chunks long it can lose: 4 sequences of up to 2000, 4 kv heads, 12.2, 10.8.
+  const auto room = [&](int shift) { return items << shift <= (shift == 3 ? 96 : shift == 2 ? 128 : kTokenBlocks); };
+  p.shift = 0;
+  while (per_item > P::kWarps && p.shift < 3 && room(p.shift + 1)) ++p.shift;
+  if (room(p.shift) && per_item <= (int64_t)3 * P::kWarps << p.shift) return launch_token<D, kType, HT, true>(p, items << p.shift, stream);
+  p.shift = 0;
+  // a chunk for each of a block's warps; up to 32 sequences may be cut item by item
+  const int64_t grid = std::min<int64_t>(kTokenBlocks, p.S <= 32 ? items * ((per_item + P::kWarps - 1) / P::kWarps) : (most + P::kWarps - 1) / P::kWarps);
+  return launch_token<D, kType, HT, false>(p, std::max<int64_t>(grid, 1), stream);
 }
 
 template <int D>

@@ -303,6 +303,26 @@ def test_token_attention(kind, Hq, Hkv, d, page, lens):
     _check_token(pool, q, lens, out, lse, d ** -0.5)
 
 
+@pytest.mark.parametrize("kind,d", [("bf16", 128), ("f32", 64), ("e4m3", 128)])
+@pytest.mark.parametrize("S,Hkv,group,longest", [(1, 4, 7, 4096), (3, 4, 2, 520), (2, 16, 1, 700), (5, 12, 1, 260), (1, 1, 20, 1500), (40, 2, 4, 100), (37, 4, 1, 30)])
+def test_short_sequences_in_short_and_in_long_tables(kind, d, S, Hkv, group, longest):
+    # blocks are dealt to the sequences' heads by what a sequence may have, or, with room for far more, by what it has
+    lens = [longest, 0, 1, longest // 2, 17, 33, longest // 3][:S] + [longest - s for s in range(max(S - 7, 0))]
+    pool = Pool(kind, lens, Hkv, d, 16, seed=S, fill=lens)
+    gen = torch.Generator(device=DEV).manual_seed(S)
+    q = _rnd(gen, S, Hkv * group, d, dtype=pool.dtype)
+    for columns in (0, 5000):
+        if columns:
+            table = torch.full((S, columns), -1, dtype=torch.int32, device=DEV)
+            table[:, :pool.table.shape[1]] = pool.table
+            pool.cache = B.make_paged_cache(pool.pages["k"], pool.pages["v"], table, pool.scale["k"], pool.scale["v"])
+        out, lse, status = _token(pool, q, _i32(lens), d ** -0.5)
+        assert status.item() == 0
+        _check_token(pool, q, lens, out, lse, d ** -0.5, only=set(range(10)))
+        again, lse2, _ = _token(pool, q, _i32(lens), d ** -0.5)
+        assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32", "e4m3"])
 def test_one_long_sequence_is_cut_and_joined(kind):
     # one sequence over all blocks; the largest scores lie in one stretch, so that the others' parts weigh nothing
