@@ -5,9 +5,10 @@
 // serves to keep loads in flight and the work behind them short.
 //   split   : the keys of all sequences and heads are laid end to end in chunks of 4 KB of K and 4 KB of V (16 keys of 128 bf16) and cut over
 //             the blocks, one per SM, evenly or item by item (an item: a sequence and a tile of the heads that share one of its kv
-//             heads), by the device from the lengths, or, where the caches are short, by the host: a cluster of blocks for every item.  A block's warps take an even stretch of its chunks each, and walk it without waiting for one another.
-//   queue   : every warp has its next chunk on the way to shared memory while it works on one (cp.async): 12 warps, 96 KB per SM.  (16 warps
-//             with fewer registers: spills; 2 blocks of 8 warps: slower by 3-5 %, another round of joins.)
+//             heads), by the device from the lengths, or, where the caches are short, by the host: a cluster of blocks for every item.  A
+//             block's warps take an even stretch of its chunks each, and walk it without waiting for one another.
+//   queue   : every warp has its next chunk on the way to shared memory while it works on one (cp.async): 12 warps, 96 KB per SM.  (2
+//             sequences of 131072 rows: 12 warps 89.1 us, 16 with fewer registers 92.5, 8 91.4; 64 ragged ones in e4m3: 78.3, 80.7, 85.7.)
 //   products: mma.sync m16n8k16 with K (16 keys) or V^T (16 dimensions) as the 16 rows and the heads as the 8 columns: no part of a product is
 //             wasted on 8 heads, and O takes 32 registers.  Which dimensions a step of the contraction takes is arbitrary as long as q is
 //             laid out alike: lane (g, t) = (lane / 4, lane % 4) reads 16 bytes of keys g and g + 8 at offset 64 c + 16 t, and these bytes
@@ -261,8 +262,8 @@ __device__ __forceinline__ float4 peer_float4(const float* p, int rank) {
   return x;
 }
 // What follows the loop where an item has 2^shift blocks of its own, a cluster: the warps' parts meet in the block's shared memory, the
-// blocks' are read from one another's.  (Joining 4 blocks
-// through the workspace, with the cut on the device, takes 2.3 us more: 1 sequence of 768 rows, 32 heads 8.8 us, 6.5 so.)
+// blocks' are read from one another's.  (1 sequence of 768 rows, 32 heads, 4 blocks each: 6.5 us; cut by the device and joined through the
+// workspace 8.8.)
 template <int D, int kType, int HT>
 __device__ __noinline__ void join_cluster(const TokenParams& p, uint8_t* dynamic, TokenShared<D, kType, HT>& sh) {
   using P = TokenPlan<D, kType, HT>;
