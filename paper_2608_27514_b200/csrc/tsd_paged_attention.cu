@@ -326,7 +326,9 @@ __device__ __noinline__ void join_parts(const TokenParams& p, uint8_t* dynamic, 
   constexpr int NW = P::kWarps;
   constexpr unsigned full = 0xffffffffu;
   // the shuffle tells the compiler that the warp branches together, a third of this function's code
-  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, x0 = sh.x0, x1 = sh.x1, each = sh.each, more = sh.more;
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  __syncthreads();  // the share that thread 0 has written, the warps' parts: a warp without chunks has come here at once
+  const int x0 = sh.x0, x1 = sh.x1, each = sh.each, more = sh.more;
   auto& part_m = sh.part_m;
   auto& part_l = sh.part_l;
   auto& part_item = sh.part_item;
@@ -344,7 +346,6 @@ __device__ __noinline__ void join_parts(const TokenParams& p, uint8_t* dynamic, 
   // ---- the block's parts: put together where they are of one sequence, then written out, or, where other blocks have the rest, to the workspace
   auto together = [&](unsigned of, int row, float& top, float& sum, float4& o) { parts_together<D, kType, HT>(sh, dynamic, of, row, top, sum, o); };
   auto write_row = [&](const Item& item, int row, float top, float sum, const float4& o) { write_row_of<D, kType>(p, item, row, top, sum, o); };
-  __syncthreads();
   int shared0 = 0, shared1 = 0, n_shared = 0;  // parts with which items of several blocks begin in this one: at most two
   {
     const bool there = lane < 2 * NW && part_item[lane].n > 0;

@@ -370,6 +370,31 @@ def test_few_sequences_among_many_slots(S, every, longest):
     _check_token(pool, q, lens, out, lse, 0.125, only=set(some[:60] + some[-5:]))
 
 
+@pytest.mark.parametrize("kind,Hkv,lens", [("bf16", 2, [9 * 16 + 5, 0, 3, 40]), ("bf16", 1, [5, 0, 0, 1]), ("f32", 3, [70, 9, 0, 130]), ("e4m3", 4, [33, 600, 0, 1])])
+def test_blocks_with_fewer_chunks_than_warps(kind, Hkv, lens):
+    # a long table (cut on the device) and few keys: most warps have no chunk, and reach the joining of parts long before the others.  A call
+    # of other lengths in between leaves another share in a block's shared memory; every call gives the same bits and leaves every ticket at 0.
+    pool = Pool(kind, lens, Hkv, 128, 16, fill=lens)
+    table = torch.full((len(lens), 6000), -1, dtype=torch.int32, device=DEV)
+    table[:, :pool.table.shape[1]] = pool.table
+    pool.cache = B.make_paged_cache(pool.pages["k"], pool.pages["v"], table, pool.scale["k"], pool.scale["v"])
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    q = _rnd(gen, len(lens), 4 * Hkv, 128, dtype=pool.dtype)
+    ws = torch.zeros(B.tsd_paged_attention_workspace_bytes(pool.cache, 4 * Hkv), dtype=torch.uint8, device=DEV)
+    out, lse, status = _token(pool, q, _i32(lens), 0.09, ws)
+    assert status.item() == 0
+    _check_token(pool, q, lens, out, lse, 0.09)
+    other = [max(n // 2, 1) if n else 0 for n in lens]
+    half, half_lse, _ = _token(pool, q, _i32(other), 0.09, ws)
+    _check_token(pool, q, other, half, half_lse, 0.09)
+    calls = [(_i32(lens), out, lse), (_i32(other), half, half_lse)]
+    for i in range(200):
+        n, o, l = calls[i % 2]
+        again, lse2, _ = _token(pool, q, n, 0.09, ws)
+        assert torch.equal(o, again) and torch.equal(l, lse2)
+    assert not ws[:148 * 4].any()
+
+
 @pytest.mark.parametrize("kind,Hq,Hkv", [("bf16", 8, 8), ("bf16", 20, 1), ("f32", 4, 2)])
 def test_scores_of_minus_infinity_weigh_nothing(kind, Hq, Hkv):
     # the first chunks of one sequence, whole stretches of another, all but the last key of a third; every key of the fourth (0 / 0)

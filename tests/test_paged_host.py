@@ -1,5 +1,7 @@
 """What the calls on a paged cache refuse, checked on the host: nothing is launched, so no GPU is needed."""
 import ctypes
+import os
+import re
 
 import pytest
 import torch
@@ -162,3 +164,15 @@ def test_results_that_would_meet_and_sizes_at_the_limit(lib):
     assert need(page_size=1024, max_pages=(1 << 21) - 3, table_stride=1 << 21) == 0
     assert need(page_size=8, max_pages=(1 << 28) - 512, table_stride=1 << 28) > 0
     assert need(page_size=8, max_pages=(1 << 28) - 511, table_stride=1 << 28) == 0
+
+
+def test_what_a_block_hands_on_is_read_behind_a_barrier():
+    # A warp without chunks comes to the joining functions at once: in front of their first block barrier they may look at nothing that
+    # another warp writes to shared memory.  Read in the source, since on a GPU the window is too narrow to be met.
+    csrc = os.path.join(os.path.dirname(os.path.abspath(B.__file__)), "csrc", "tsd_paged_attention.cu")
+    with open(csrc) as f:
+        code = re.sub(r"//[^\n]*", "", f.read())
+    for name in ("join_cluster", "join_parts"):
+        body = code.split("void %s(" % name, 1)[1].split("\n}\n", 1)[0].split("{", 1)[1]
+        before, barrier, _ = body.partition("__syncthreads();")
+        assert barrier and not re.search(r"\bsh\.", before), name
