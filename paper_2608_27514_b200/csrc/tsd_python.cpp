@@ -472,12 +472,20 @@ T* vec(PyObject* o, int64_t count, const Here& here, const char* what) {
   want(t.is(std::is_same<T, float>::value ? kDLFloat : kDLInt, 32) && t.contiguous() && t.count() == count, what);
   return static_cast<T*>(t.data());
 }
-// any tensor or None: its address, its bytes
-void* memory(PyObject* o, const Here& here, size_t* bytes = nullptr) {
+// any tensor whose elements lie without gaps, or None: its address, its bytes
+void* memory(PyObject* o, const Here& here, size_t* bytes, const char* what) {
   if (o == Py_None) return nullptr;
   const Tensor t(o, here);
-  if (bytes) *bytes = (size_t)t.count() * t.t.dtype.bits / 8;
+  want(t.contiguous(), what);
+  *bytes = (size_t)t.count() * t.t.dtype.bits / 8;
   return t.data();
+}
+// the word in which a kernel reports, or None
+uint32_t* status_word(PyObject* o, const Here& here) {
+  if (o == Py_None) return nullptr;
+  const Tensor t(o, here);
+  want((t.is(kDLInt, 32) || t.is(kDLUInt, 32)) && t.count() > 0, "status is an int32 or uint32 tensor of an element at least");
+  return static_cast<uint32_t*>(t.data());
 }
 struct Rows {  // [batch, rows, heads, dim], dim contiguous
   int64_t n[4], st[4];
@@ -556,7 +564,7 @@ PyObject* append_paged(Args a) {
     t.inv_freq = vec<float>(a[6], pairs, here, "inv_freq is a contiguous fp32 [rotary_dim / 2]");
   }
   t.interleaved = PyObject_IsTrue(a[7]);
-  t.status = static_cast<uint32_t*>(memory(a[13], here));
+  t.status = status_word(a[13], here);
   if (a[0] == Py_None) return done(call(tsd_append_paged_kv, &t, here.stream(a[14])), "tsd_append_paged_kv");
   const Pages cache(a[0], here);
   t.cache = cache.get();
@@ -577,11 +585,11 @@ PyObject* paged_attention(Args a) {
   const int32_t dtype = tq.model_type(a[1]);
   want(to.model_type(a[3]) == dtype, "types of q and out differ");
   size_t bytes = 0;
-  void* const workspace = memory(a[6], here, &bytes);
+  void* const workspace = memory(a[6], here, &bytes, "the workspace is contiguous");
   return done(call(tsd_paged_attention, cache.get(), small(q[1]), dtype, tq.data(), qs[0], qs[1],
                    vec<int32_t>(a[2], q[0], here, "kv_lens is a contiguous int32 [sequences]"), to.data(), os[0], os[1],
                    vec<float>(a[4], q[0] * q[1], here, "lse is a contiguous fp32 [sequences, heads]"), to_float(a[5]), workspace, bytes,
-                   static_cast<uint32_t*>(memory(a[7], here)), here.stream(a[8])),
+                   status_word(a[7], here), here.stream(a[8])),
               "tsd_paged_attention");
 }
 
@@ -600,13 +608,13 @@ PyObject* verify_attention_paged(Args a) {
   v.along(k);
   o.as(q, true);
   size_t mask_bytes = 0, bytes = 0;
-  const void* const mask = memory(a[1], here, &mask_bytes);
-  void* const workspace = memory(a[9], here, &bytes);
+  const void* const mask = memory(a[1], here, &mask_bytes, "the mask is contiguous");
+  void* const workspace = memory(a[9], here, &bytes, "the workspace is contiguous");
   want(mask && mask_bytes >= tsd_branch_mask_bytes(l), "the mask is that of the layout");
   return done(call(tsd_verify_attention_paged, l, mask, q.data, q.st[0], q.st[1], q.st[2], cache.get(), k.data, v.data, k.st[0], k.st[1],
                    k.st[2], o.data, o.st[0], o.st[1], o.st[2],
                    vec<float>(a[7], q.n[0] * q.n[1] * q.n[2], here, "lse is a contiguous fp32 [batch, heads, rows]"), to_float(a[8]), workspace,
-                   bytes, (uint32_t)to_int(a[10]), static_cast<uint32_t*>(memory(a[11], here)), here.stream(a[12])),
+                   bytes, (uint32_t)to_int(a[10]), status_word(a[11], here), here.stream(a[12])),
               "tsd_verify_attention_paged");
 }
 

@@ -645,6 +645,39 @@ def test_refusals_of_the_binding():
         B.tsd_append_paged_kv(pool.cache, k, None)
 
 
+def test_status_and_workspace_are_checked():
+    # refused before anything is launched: a kernel reports with a 32-bit atomic, and counts on every byte of a workspace or a mask
+    pool = Pool("bf16", [64, 64], 2, 128, 16)
+    q, k = [torch.zeros((2, 6, h, 128), dtype=torch.bfloat16, device=DEV) for h in (4, 2)]
+    ws = torch.zeros(B.tsd_paged_attention_workspace_bytes(pool.cache, 4), dtype=torch.uint8, device=DEV)
+    step = VerifyStep(2, 1, 32, 64, 4, 2, 128, 64, 1, torch.bfloat16)
+    step.build_mask()
+    qv, kv = [torch.zeros((2, 32, h, 128), dtype=torch.bfloat16, device=DEV) for h in (4, 2)]
+    out, lse = torch.empty_like(q[:, 0]), torch.empty((2, 4), device=DEV)
+
+    def calls(status=None, workspace=ws, mask=step.mask):
+        return (lambda: B.tsd_append_paged_kv(pool.cache, k, k, status=status),
+                lambda: B.tsd_paged_attention(pool.cache, q[:, 0], None, out, lse, 0.1, workspace, status),
+                lambda: B.tsd_verify_attention_paged(step.layout, mask, qv, pool.cache, kv, kv, step.out, None, 0.1, workspace, 0, status))
+
+    for status in (torch.zeros(1, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV).view(torch.uint32),
+                   torch.zeros(3, dtype=torch.int32, device=DEV), None):
+        for call in calls(status):
+            call()
+    one = torch.zeros(8, dtype=torch.uint8, device=DEV)
+    for status in (one[:1], one[1:5], one[:0].view(torch.int32), torch.zeros(1, dtype=torch.int64, device=DEV), torch.zeros(1, device=DEV),
+                   torch.zeros(1, dtype=torch.int32)):
+        for call in calls(status):
+            with pytest.raises(AssertionError):
+                call()
+    with pytest.raises(AssertionError):
+        calls(workspace=ws[:1].expand(len(ws)))[1]()
+    with pytest.raises(AssertionError):
+        calls(workspace=torch.zeros(2 * len(ws), dtype=torch.uint8, device=DEV)[::2])[1]()
+    with pytest.raises(AssertionError):
+        calls(mask=step.mask.view(torch.uint8)[:1].expand(step.mask.nbytes))[2]()
+
+
 # ---------------------------------------------------------------------------------------- together
 def test_a_block_from_prompt_to_next_token():
     """Prompts into pages, a tree's rows rotated, verified over the pages, its accepted node appended, and a token on top: every stage
