@@ -138,6 +138,9 @@ append_kernel(const T* k, const T* v, const T* q, T* k_out, T* q_out, AppendPara
   // A unit's two chunks of 8: dimensions [place * 8, + 8) and [D / 2 + place * 8, + 8).  Halves of rot < D dimensions that rotate into each other
   // are closer: the first rot / 16 places take these, the others 16 neighbours behind them.
   const bool closer = !kNext && p.rot > 0 && p.rot < D, turning = kNext ? place * 8 < p.rot : place * 16 < p.rot;
+  // Neighbours: the second chunk lies behind rot before the first one does, and what lies there is copied (times a turn of 0 an infinity
+  // would make its neighbour NaN).
+  const bool both = D / 2 + place * 8 < p.rot;
   const int d0_rot = closer && !turning ? place * 16 : place * 8, d1_rot = !closer ? D / 2 + place * 8 : turning ? half + place * 8 : place * 16 + 8;
   const int heads = p.Hq + p.Hkv + (p.cached ? p.Hkv : 0);
 
@@ -273,8 +276,10 @@ append_kernel(const T* k, const T* v, const T* q, T* k_out, T* q_out, AppendPara
             const float x0 = x[2 * j], x1 = x[2 * j + 1], y0 = y[2 * j], y1 = y[2 * j + 1];
             x[2 * j] = x0 * a.x - x1 * a.y;
             x[2 * j + 1] = x0 * a.y + x1 * a.x;
-            y[2 * j] = y0 * b.x - y1 * b.y;
-            y[2 * j + 1] = y0 * b.y + y1 * b.x;
+            if (both) {
+              y[2 * j] = y0 * b.x - y1 * b.y;
+              y[2 * j + 1] = y0 * b.y + y1 * b.x;
+            }
           }
         } else {
 #pragma unroll

@@ -149,6 +149,41 @@ def test_append(kind, interleaved, S, n, Hq, Hkv, d, page, rot, start, ragged):
 
 
 @pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("kind", ["bf16", "f32", "e4m3"])
+@pytest.mark.parametrize("d,rot", [(128, 16), (128, 48), (128, 64), (128, 112), (64, 16), (64, 32), (64, 48), (128, 0)])
+def test_dimensions_that_do_not_turn_are_copied(d, rot, kind, interleaved):
+    # behind rotary_dim there may be anything: infinities, NaN and zeros of both signs come out as they are, and the dimensions that turn
+    # are those of a call without them, bit for bit
+    gen = torch.Generator(device=DEV).manual_seed(rot + d)
+    dt, n = TYPES[kind][0], 11
+    k, v, q = _rnd(gen, 2, n, 2, d, dtype=dt), _rnd(gen, 2, n, 2, d, dtype=dt), _rnd(gen, 2, n, 6, d, dtype=dt)
+    freq = (1e4 ** (-torch.arange(0, rot, 2, device=DEV) / max(rot, 1))).float() if rot else None
+    odd = torch.tensor([float("inf"), -0.0, -float("inf"), 1.5, float("nan"), -0.0, -2.5, 0.0, -0.0, -1.0], dtype=dt, device=DEV)
+
+    def run(k, q):
+        pool = Pool(kind, [n, n], 2, d, 16, seed=1)
+        outs = [torch.zeros_like(q), torch.zeros_like(k)]
+        B.tsd_append_paged_kv(pool.cache, k, v, inv_freq=freq, interleaved=interleaved, q=q, q_out=outs[0], k_out=outs[1])
+        at = pool.table[:, 0].long()
+        return outs + [pool.codes("k")[at][:, :n]]
+
+    def same(a, b):
+        bits = {1: torch.uint8, 2: torch.int16, 4: torch.int32}[a.element_size()]
+        return bool(((a.view(bits) == b.view(bits)) | ((a != a) & (b != b))).all())
+
+    plain = run(k, q)
+    k2, q2 = k.clone(), q.clone()
+    for x in (k2, q2):
+        x[..., rot:] = odd[torch.randint(0, len(odd), x[..., rot:].shape, generator=gen, device=DEV)]
+    got = run(k2, q2)
+    for a, b in zip(got, plain):
+        assert same(a[..., :rot].contiguous(), b[..., :rot].contiguous())
+    assert same(got[0][..., rot:].contiguous(), q2[..., rot:].contiguous()) and same(got[1][..., rot:].contiguous(), k2[..., rot:].contiguous())
+    freq = None                                                                         # the pages hold what a call without rotation puts there
+    assert same(got[2][..., rot:].contiguous(), run(k2, q2)[2][..., rot:].contiguous())
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
 def test_far_and_negative_positions(interleaved):
     # positions whose angle fp32 does not hold, and a frequency that makes the angle pass 2^32 quarters
     pos = [[1 << 20, 999983, 131071], [0x7fffffff, -1, -131071]]
