@@ -184,6 +184,63 @@ def test_dimensions_that_do_not_turn_are_copied(d, rot, kind, interleaved):
 
 
 @pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("kind", ["bf16", "f32", "e4m3"])
+@pytest.mark.parametrize("S,n,blocks,Hq,Hkv,d,page,rot", [(40, 131, 1, 6, 2, 128, 16, 128), (45, 120, 2, 28, 4, 64, 64, 32), (32, 160, 3, 4, 1, 128, 32, 112),
+                                                          (30, 217, 1, 12, 3, 64, 8, 64), (3, 1901, 1, 8, 8, 128, 128, 128)])
+def test_append_of_more_rows_than_warps(kind, interleaved, S, n, blocks, Hq, Hkv, d, page, rot):
+    # A warp takes several rows, each of a position and a sequence of its own, the next ones under way while it turns one: more rows than twice
+    # the warps.  Rows that do not count, sequences without any and blocks that do not exist lie in between, up to 32 sequences and more.
+    rng = np.random.default_rng(S + n)
+    new = [int(x) for x in rng.integers(n // 2, n + 1, S)]
+    new[1::5] = [0] * len(new[1::5])
+    new[-1] = n + 9
+    start = [int(x) for x in rng.integers(0, 3 * page, S)]
+    block = [int(x) for x in rng.integers(0, blocks, S)]
+    if blocks > 1:
+        block[2::9] = [blocks, -1, 1 << 30, -(1 << 31), blocks][:len(block[2::9])]
+    count = [min(m, n) if 0 <= b < blocks else 0 for m, b in zip(new, block)]
+    assert S * n > 2 * 2368
+    gen = torch.Generator(device=DEV).manual_seed(n)
+    dt, ct = TYPES[kind]
+    pool = Pool(kind, [a + n for a in start], Hkv, d, page, seed=2)
+    k, v, q = [_rnd(gen, S, blocks * n, h, d, dtype=dt) for h in (Hkv, Hkv, Hq)]
+    pos = torch.randint(0, 100000, (S, n), generator=gen, device=DEV, dtype=torch.int32)
+    freq = (1e4 ** (-torch.arange(0, rot, 2, device=DEV) / rot)).float()
+    before = {x: pool.codes(x) for x in "kv"}
+    q_out, k_out = torch.full_like(q, 7.0), torch.full_like(k, 7.0)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.tsd_append_paged_kv(pool.cache, k, v, _i32(start), _i32(new), pos, freq, interleaved, q, q_out, k_out, _i32(block) if blocks > 1 else None, n, status)
+    assert (status.item() != 0) == (blocks > 1)
+    f, where, table = _np(freq), pos.cpu().numpy(), pool.table.cpu().numpy()
+    touched = torch.zeros(pool.pages["k"].shape[:2], dtype=torch.bool, device=DEV)
+    left = {"q": torch.ones(q.shape[:2], dtype=torch.bool, device=DEV), "k": torch.ones(q.shape[:2], dtype=torch.bool, device=DEV)}
+    for s, m in enumerate(count):
+        if m == 0:
+            continue
+        rows = slice(block[s] * n, block[s] * n + m)
+        at = oracle.slots(start[s], m, table[s], page, pool.cache.n_pages)
+        pages, lines = [torch.tensor([a[i] for a in at], dtype=torch.long, device=DEV) for i in (0, 1)]
+        touched[pages, lines] = True
+        for x, out, name in ((q, q_out, "q"), (k, k_out, "k"), (v, None, "v")):
+            here = _np(x[s, rows])
+            ref = here if name == "v" else oracle.rotate(here, where[s, :m], f, interleaved)
+            size = _pair_size(here, 0 if name == "v" else len(f), interleaved)
+            if out is not None:
+                _check_rotated(_np(out[s, rows]), ref, size, dt)
+                left[name][s, rows] = False
+            if name == "q":
+                continue
+            if kind == "e4m3":
+                sc = _np(pool.scale[name])[None, :, None]
+                ref, size = np.clip(ref / sc, -448, 448), size / sc
+            got = _np(pool.pages[name].view(torch.uint8)[pages, lines].view(FP8) if kind == "e4m3" else pool.pages[name][pages, lines])
+            _check_rotated(got, ref, size, ct)
+    assert bool((q_out[left["q"]] == 7).all()) and bool((k_out[left["k"]] == 7).all())
+    for x in "kv":
+        assert torch.equal(pool.codes(x)[~touched], before[x][~touched])
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
 def test_far_and_negative_positions(interleaved):
     # positions whose angle fp32 does not hold, and a frequency that makes the angle pass 2^32 quarters
     pos = [[1 << 20, 999983, 131071], [0x7fffffff, -1, -131071]]
