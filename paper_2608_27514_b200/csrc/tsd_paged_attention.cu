@@ -1,6 +1,6 @@
 // Attention of one new token per sequence over a paged K/V cache (no counterpart in the paper, whose passes verify whole blocks:
 // tsd_verify_attention).  With q the query rows of the heads that share a kv head,
-//     s_t = sm_scale <q, k_t>,   out = sum_t e^(s_t - m) v_t / sum_t e^(s_t - m),   m >= max_t s_t - 8 log 2.
+//     s_t = sm_scale <q, k_t>,   out = sum_t e^(s_t - m) v_t / sum_t e^(s_t - m),   m >= max_t s_t - 8 log 2 (8-bit values: - 15).
 // Every cached row is read once and used for a few multiply-adds per head, so the kernel is bound by memory; everything in it
 // serves to keep loads in flight and the work behind them short.
 //   split   : the keys of all sequences and heads are laid end to end in chunks of 4 KB of K and 4 KB of V (16 keys of 128 bf16) and cut over
@@ -14,9 +14,10 @@
 //             laid out alike: lane (g, t) = (lane / 4, lane % 4) reads 16 bytes of keys g and g + 8 at offset 64 c + 16 t, and these bytes
 //             are the operand as they are.  For V^T the lane reads columns 8 g ... of keys 2t, 2t+1, 2t+8, 2t+9 and pairs the keys'
 //             halves (a byte permutation per register).  Weights go from the one layout to the other by movmatrix, in two
-//             16-bit parts (high, residual: 2^-17 relative).  8-bit codes become f16, one conversion per pair.  The tensor-memory
-//             instructions would want 128 rows, and the scores back through tensor memory.
-//   offset  : m moves only when a score passes it by 8 (in the exp2 domain): one vote per chunk instead of a reduction.
+//             16-bit parts (high, residual: off by 2^-17 of the weight; for 8-bit values, f16 parts, by 2^-22 of it and 2^-32 of the largest
+//             one).  8-bit codes become f16, one conversion per pair.  The tensor-memory instructions would want 128 rows, and the scores back
+//             through tensor memory.
+//   offset  : m moves only when a score passes it by 8 (in the exp2 domain; 8-bit values: 15): one vote per chunk instead of a reduction.
 //   fp32    : the same queue on CUDA cores (the scores' partial sums of a key meet over its 4 lanes, the weights in shared memory).
 //   join    : an item that a warp has from its first chunk to its last is written out at once.  Otherwise the warps' offsets, sums and rows meet
 //             in shared memory, and what is not the whole of its item goes to the workspace: the last of the item's blocks to
@@ -40,7 +41,12 @@ constexpr int kTokenBlocks = kPlanSms;  // at most: what the workspace is sized 
 constexpr int kAlignSlack = 4;          // the part of a share by which it may grow to keep items apart
 constexpr int kReadPast = 4096;         // chunks: 32 MB, a quarter of L2
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kSlack = 8.f;           // by how much a score may pass the offset, as a power of 2
+constexpr float kSlack = 8.f;           // by how much a score may pass what the offset was set by, as a power of 2
+// How far below the largest score the offset is set, as a power of 2.  The weights of 8-bit values are two f16 parts, and f16 ends at 2^-24:
+// with the largest weight at 2^7 or above what is lost of a weight is 2^-32 of that one (at 1, 2^-25: keys 17.5 nats below another were in the
+// sum of weights, but not in that of the values).  2^(7 + 8) is still an f16.
+template <int kType>
+constexpr float kBelow = kType == TSD_E4M3 ? 7.f : 0.f;
 constexpr float kLowest = -FLT_MAX;     // the first offset: finite, so that a score of -infinity has the weight 0 from the first key on
 
 enum { kTypeF32 = TSD_F32, kTypeBf16 = TSD_BF16, kTypeE4m3 = TSD_E4M3 };
@@ -959,7 +965,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) token
           top[i] = -CUDART_INF_F;
 #pragma unroll
           for (int mt = 0; mt < NG / 2; ++mt) top[i] = fmaxf(top[i], fmaxf(sc[mt][i >> 1][i & 1], sc[mt][i >> 1][2 + (i & 1)]));
-          passed |= top[i] > m[i] + kSlack;
+          passed |= top[i] > m[i] + (kBelow<kType> + kSlack);
         }
         if (__any_sync(full, passed)) {
 #pragma unroll
@@ -967,7 +973,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) token
             top[i] = fmaxf(top[i], __shfl_xor_sync(full, top[i], 4));
             top[i] = fmaxf(top[i], __shfl_xor_sync(full, top[i], 8));
             top[i] = fmaxf(top[i], __shfl_xor_sync(full, top[i], 16));
-            const float to = fmaxf(m[i], top[i]);
+            const float to = fmaxf(m[i], top[i] - kBelow<kType>);
             const float alpha = m[i] == to ? 1.f : exp2_approx(m[i] - to);
             m[i] = to;
             l[i] *= alpha;

@@ -487,6 +487,38 @@ def test_blocks_with_fewer_chunks_than_warps(kind, Hkv, lens):
     assert not ws[:148 * 4].any()
 
 
+@pytest.mark.parametrize("S,Hkv,group,d,n,at", [(64, 32, 1, 128, 1000, 0), (64, 32, 1, 64, 1000, 999), (40, 4, 8, 128, 5000, 2500), (3, 2, 16, 64, 3000, 0)])
+@pytest.mark.parametrize("gap", [9.0, 14.0, 17.5, 18.5, 21.0, 30.0])
+def test_e4m3_weights_far_below_the_largest(S, Hkv, group, d, n, at, gap):
+    # One key `gap` nats above all others, whose value is 0: what the others come to is all there is.  Scores are 0 and gap, as exact as fp32 has
+    # them: a weight is off by 8 u gap (scale, its factor log2 e, subtraction) and 2^-21 (exp2), relatively, an output of values
+    # >= 0 by twice that and its own rounding; and by the weights' split, 2^-22 and, a f16 ending at 2^-24 and the largest weight of a warp
+    # being 2^7 at least, 2^-32 of the largest per key.
+    pool = Pool("e4m3", [n] * S, Hkv, d, 64)
+    pool.scale["k"].fill_(gap / 256)
+    pool.scale["v"].fill_(1.0)
+    k, v = pool.pages["k"], pool.pages["v"]
+    k.view(torch.uint8).zero_()
+    v.view(torch.uint8).bitwise_and_(0x7F).clamp_(max=0x60)
+    v[..., 0] = torch.tensor(1.0).to(FP8)
+    page = pool.table[:, at // 64].long()
+    k[page, at % 64, :, 0] = torch.tensor(256.0).to(FP8)
+    v.view(torch.uint8)[page, at % 64] = 0
+    q = torch.zeros((S, Hkv * group, d), dtype=torch.bfloat16, device=DEV)
+    q[:, :, 0] = 1.0
+    out, lse, _ = _token(pool, q, _i32([n] * S), 1.0)
+    small = float(np.exp(np.float64(-np.float32(gap / 256) * np.float64(256))))
+    total = 1.0 + (n - 1) * small
+    off = 8 * 2.0 ** -24 * gap + 2.0 ** -21
+    for s in {0, S // 2, S - 1}:
+        rows = torch.arange(n, device=DEV)
+        values = _np(v[pool.table[s, rows // 64].long(), rows % 64])
+        ref = np.repeat(values.sum(0) * small / total, group, 0)
+        tol = (2.0 ** -8 + 2 * off) * ref + (2.0 ** -22 + n * 2.0 ** -32) * values.max()
+        assert (np.abs(_np(out[s]) - ref) <= tol).all(), (np.abs(_np(out[s]) - ref) / tol).max()
+        assert np.abs(_np(lse[s]) - (gap + np.log(total))).max() <= off + 2.0 ** -22 * (1 + gap)
+
+
 @pytest.mark.parametrize("kind,Hq,Hkv", [("bf16", 8, 8), ("bf16", 20, 1), ("f32", 4, 2)])
 def test_scores_of_minus_infinity_weigh_nothing(kind, Hq, Hkv):
     # the first chunks of one sequence, whole stretches of another, all but the last key of a third; every key of the fourth (0 / 0)
