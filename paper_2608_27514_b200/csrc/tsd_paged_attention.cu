@@ -560,8 +560,9 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) token
     int item_blocks = 0, in_item = 0;  // of the block's item, if they are cut one by one: blocks, and which of them this is
     int pieces = 0;                         // of each item of the lane's sequence
     if (a.S <= 32 && total > 0) {
-      auto fit = [&](int piece) {  // a quotient that is off by a rounding is as good: what counts is the pieces' number
-        pieces = n0 > 0 ? max(1, (int)ceilf(__fdividef((float)n0, (float)piece))) : 0;
+      // A quotient that is off by a rounding is as good, as long as no piece is empty: a block without chunks would never arrive.
+      auto fit = [&](int piece) {
+        pieces = min(n0, max(1, (int)ceilf(__fdividef((float)n0, (float)piece))));
         return HI * __reduce_add_sync(full, pieces) <= most_blocks;
       };
       int lo = each + (more > 0) - 1, hi = each + 2 + each / kAlignSlack;  // the smallest that fits is looked for in (lo, hi]

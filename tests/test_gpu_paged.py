@@ -487,6 +487,22 @@ def test_blocks_with_fewer_chunks_than_warps(kind, Hkv, lens):
     assert not ws[:148 * 4].any()
 
 
+@pytest.mark.parametrize("kind,keys", [("bf16", 16), ("f32", 8), ("e4m3", 32)])
+def test_items_of_one_chunk_each(kind, keys):
+    # the smallest pieces there are, cut on the device: each is the whole of its item, so that no ticket is ever drawn
+    lens = [keys, 1, 0, keys - 1, keys, 3, 0, keys]
+    pool = Pool(kind, lens, 5, 128, 8, fill=lens)
+    table = torch.full((len(lens), 6000), -1, dtype=torch.int32, device=DEV)
+    table[:, :pool.table.shape[1]] = pool.table
+    pool.cache = B.make_paged_cache(pool.pages["k"], pool.pages["v"], table, pool.scale["k"], pool.scale["v"])
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    q = _rnd(gen, len(lens), 10, 128, dtype=pool.dtype)
+    ws = torch.zeros(B.tsd_paged_attention_workspace_bytes(pool.cache, 10), dtype=torch.uint8, device=DEV)
+    out, lse, status = _token(pool, q, _i32(lens), 0.09, ws)
+    assert status.item() == 0 and not ws.any()
+    _check_token(pool, q, lens, out, lse, 0.09)
+
+
 @pytest.mark.parametrize("S,Hkv,group,d,n,at", [(64, 32, 1, 128, 1000, 0), (64, 32, 1, 64, 1000, 999), (40, 4, 8, 128, 5000, 2500), (3, 2, 16, 64, 3000, 0)])
 @pytest.mark.parametrize("gap", [9.0, 14.0, 17.5, 18.5, 21.0, 30.0])
 def test_e4m3_weights_far_below_the_largest(S, Hkv, group, d, n, at, gap):
