@@ -141,7 +141,7 @@ def native():
         except ImportError as e:
             raise RuntimeError("_tsd_native.so is missing: build it with `python -m paper_2608_27514_b200.build`") from e
         _tsd_native.setup(torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch.float32, torch.bfloat16, TsdError, torch.Tensor,
-                          torch.Tensor.__dlpack_c_exchange_api__)
+                          getattr(torch.Tensor, "__dlpack_c_exchange_api__", None))  # None: no calls on a paged cache
         _native = _tsd_native
     return _native
 

@@ -2,19 +2,27 @@
 // addresses and strides, calls libtsd.  A call through ctypes costs 10-17 us of interpreter time (argument
 // conversion, torch.cuda.current_stream()), as much as the kernels of a small pass; here it costs about 2 us plus
 // the launches.  Only the CPython API is used: tensors are asked for data_ptr(), stride(), shape and nbytes, or (the calls on
-// a paged cache) for all of it at once through torch's DLPack exchange table, a C interface.
+// a paged cache) for all of it at once through torch's DLPack exchange table, a C interface.  A torch without that table (here: DLPack
+// 1.3 at least) serves all calls but those.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <stdint.h>
 #include <type_traits>
+#if __has_include(<ATen/dlpack.h>)
 #include <ATen/dlpack.h>
+#endif
+#if defined(DLPACK_MAJOR_VERSION) && DLPACK_MAJOR_VERSION == 1 && DLPACK_MINOR_VERSION >= 3
+#define TSD_EXCHANGE_TABLE 1
+#endif
 #include "../../include/tsd.h"
 
 namespace {
 
 PyObject *n_data_ptr, *n_stride, *n_shape, *n_nbytes, *n_dtype, *n_cuda_stream, *n_is_contiguous, *n_device;
 PyObject *get_device, *get_raw_stream, *dtype_f32, *dtype_bf16, *error_type, *tensor_type;  // set by setup()
-const DLPackExchangeAPI* exchange;
+#ifdef TSD_EXCHANGE_TABLE
+const DLPackExchangeAPI* exchange;  // null: this torch has none
+#endif
 
 struct Failed {};  // a Python exception is set
 
@@ -148,14 +156,13 @@ PyObject* done(int rc, const char* where) {
 using Args = PyObject* const*;
 
 PyObject* setup(Args a) {
-  const void* table = PyCapsule_GetPointer(a[6], "dlpack_exchange_api");
-  if (!table) throw Failed{};
-  const auto* api = static_cast<const DLPackExchangeAPI*>(table);
-  if (api->header.version.major != DLPACK_MAJOR_VERSION || !api->dltensor_from_py_object_no_sync) {
-    PyErr_SetString(PyExc_RuntimeError, "torch's DLPack exchange table is of another version than the one this was built with");
-    throw Failed{};
+#ifdef TSD_EXCHANGE_TABLE
+  exchange = nullptr;
+  if (PyCapsule_IsValid(a[6], "dlpack_exchange_api")) {
+    const auto* api = static_cast<const DLPackExchangeAPI*>(PyCapsule_GetPointer(a[6], "dlpack_exchange_api"));
+    if (api->header.version.major == DLPACK_MAJOR_VERSION && api->dltensor_from_py_object_no_sync && api->current_work_stream) exchange = api;
   }
-  exchange = api;
+#endif
   PyObject** to[] = {&get_device, &get_raw_stream, &dtype_f32, &dtype_bf16, &error_type, &tensor_type};
   for (int i = 0; i < 6; ++i) {
     Py_INCREF(a[i]);
@@ -411,9 +418,14 @@ PyObject* advance_block(Args a) {
 }
 
 // ---- the calls on a paged cache check what they are given: sizes, types, and that it lies on the current device
+#ifdef TSD_EXCHANGE_TABLE
 struct Here {
   int32_t device;
   Here() {
+    if (!exchange) {
+      PyErr_SetString(PyExc_RuntimeError, "the calls on a paged cache want a torch with a DLPack exchange table of the version that this was built with");
+      throw Failed{};
+    }
     Ref d(PyObject_CallNoArgs(get_device));
     device = to_i32(d.p);
   }
@@ -617,6 +629,16 @@ PyObject* verify_attention_paged(Args a) {
                    bytes, (uint32_t)to_int(a[10]), status_word(a[11], here), here.stream(a[12])),
               "tsd_verify_attention_paged");
 }
+
+#else
+[[noreturn]] PyObject* no_table() {
+  PyErr_SetString(PyExc_RuntimeError, "the calls on a paged cache were not built: they want the headers of a torch with a DLPack exchange table");
+  throw Failed{};
+}
+PyObject* append_paged(Args) { no_table(); }
+PyObject* paged_attention(Args) { no_table(); }
+PyObject* verify_attention_paged(Args) { no_table(); }
+#endif
 
 // n_masked [S], status, report, ticket, stream
 PyObject* report_block(Args a) {

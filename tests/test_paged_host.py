@@ -2,6 +2,8 @@
 import ctypes
 import os
 import re
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -176,3 +178,36 @@ def test_what_a_block_hands_on_is_read_behind_a_barrier():
         body = code.split("void %s(" % name, 1)[1].split("\n}\n", 1)[0].split("{", 1)[1]
         before, barrier, _ = body.partition("__syncthreads();")
         assert barrier and not re.search(r"\bsh\.", before), name
+
+
+@pytest.mark.parametrize("table", ["none", "of another version"])
+def test_a_torch_without_an_exchange_table_has_the_other_calls(lib, table):
+    # only the calls on a paged cache read tensors through that table; in a process of its own, since the module keeps what it was given
+    code = """
+import ctypes, sys, torch
+from paper_2608_27514_b200 import binding as B
+B.lib()
+from paper_2608_27514_b200 import _tsd_native as N
+other = (ctypes.c_uint32 * 32)(2, 0)  # a header of version 2
+new = ctypes.pythonapi.PyCapsule_New
+new.restype, new.argtypes = ctypes.py_object, [ctypes.c_void_p, ctypes.c_char_p, ctypes.c_void_p]
+table = None if sys.argv[1] == "none" else new(ctypes.addressof(other), b"dlpack_exchange_api", None)
+N.setup(lambda: 0, lambda device: 0, torch.float32, torch.bfloat16, B.TsdError, torch.Tensor, table)
+B._native = N
+try:
+    B.tsd_build_branch_mask(B.make_layout(0, 1, 32, 0, 1, 1, 128, B.TSD_BF16), None, None, torch.zeros(64, dtype=torch.uint8))
+    raise SystemExit("an empty layout was taken")
+except B.TsdError as e:
+    assert e.code == B.TSD_ERR_INVALID_ARG, e
+x = torch.zeros((1, 1, 1, 64))
+for call in (lambda: B.tsd_append_paged_kv(None, x, None), lambda: B.tsd_paged_attention(None, x, None, x),
+             lambda: B.tsd_verify_attention_paged(None, None, x, None, x, x, x)):
+    try:
+        call()
+        raise SystemExit("a call on a paged cache was made without the table")
+    except RuntimeError as e:
+        assert "exchange table" in str(e), e
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(B.__file__)))
+    done = subprocess.run([sys.executable, "-c", code, table], cwd=root, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
