@@ -522,7 +522,7 @@ struct Rows {  // [batch, rows, heads, dim], dim contiguous
   }
 };
 int32_t small(int64_t v) {
-  want(v >= 0 && v <= 0x7fffffff, "a size is too large");
+  want(v >= 0 && v <= 0x7fffffff, "a size is negative or too large");
   return (int32_t)v;
 }
 
@@ -534,8 +534,8 @@ PyObject* append_paged(Args a) {
   t.dtype = k.dtype;
   k.to(t.kv_stride);
   t.batch = small(k.n[0]);
-  t.n_rows = a[12] == Py_None ? small(k.n[1]) : to_i32(a[12]);
-  want(t.n_rows >= 0 && (t.n_rows == 0 ? k.n[1] == 0 : k.n[1] % t.n_rows == 0), "the rows are whole blocks of n_rows");
+  t.n_rows = small(a[12] == Py_None ? k.n[1] : to_int(a[12]));
+  want(t.n_rows == 0 ? k.n[1] == 0 : k.n[1] % t.n_rows == 0, "the rows are whole blocks of n_rows");
   t.n_blocks = t.n_rows ? small(k.n[1] / t.n_rows) : 1;
   if (t.n_blocks == 0) { t.n_blocks = 1; t.n_rows = 0; }
   t.n_kv_heads = small(k.n[2]);
@@ -576,6 +576,7 @@ PyObject* append_paged(Args a) {
     t.inv_freq = vec<float>(a[6], pairs, here, "inv_freq is a contiguous fp32 [rotary_dim / 2]");
   }
   t.interleaved = PyObject_IsTrue(a[7]);
+  if (t.interleaved < 0) throw Failed{};
   t.status = status_word(a[13], here);
   if (a[0] == Py_None) return done(call(tsd_append_paged_kv, &t, here.stream(a[14])), "tsd_append_paged_kv");
   const Pages cache(a[0], here);

@@ -818,6 +818,19 @@ def test_status_and_workspace_are_checked():
         calls(mask=step.mask.view(torch.uint8)[:1].expand(step.mask.nbytes))[2]()
 
 
+def test_arguments_of_an_append_that_do_not_convert():
+    # neither a number of rows that 32 bits do not hold nor a truth value that has none reaches the call
+    k = torch.zeros((2, 6, 2, 128), dtype=torch.bfloat16, device=DEV)
+    out = torch.full_like(k, 7.0)
+    for n_rows in ((1 << 32) + 6, (1 << 32) + 3, -6, 1 << 31):
+        with pytest.raises(AssertionError):
+            B.tsd_append_paged_kv(None, k, None, k_out=out, n_rows=n_rows)
+    with pytest.raises(RuntimeError):
+        B.tsd_append_paged_kv(None, k, None, k_out=out, interleaved=torch.ones(2, dtype=torch.bool))
+    torch.cuda.synchronize()
+    assert bool((out == 7).all())
+
+
 # ---------------------------------------------------------------------------------------- together
 def test_a_block_from_prompt_to_next_token():
     """Prompts into pages, a tree's rows rotated, verified over the pages, its accepted node appended, and a token on top: every stage
