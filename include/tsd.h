@@ -680,7 +680,9 @@ int tsd_append_paged_kv(const tsd_append_args* args, tsd_stream_t stream);
  *     out[s, h] = sum_t softmax_t(sm_scale * <q[s, h], k_t>) v_t ,  t < kv_lens[s],
  * kv head h / (n_q_heads / n_kv_heads).  The new token's own key and value are in the cache already.  A sequence
  * of length 0 gives 0 and a log-sum-exp of -inf.  Rows at or past kv_lens[s] can hold anything.
- * Of the rows before: a score of -infinity weighs nothing; a value that is not finite makes its dimension of the heads that read it NaN.
+ * Of the rows before: a score of -infinity weighs nothing (if all of a row's are, 0 / 0: out is NaN, the log-sum-exp -inf); a value that is not
+ * finite makes its dimension of the heads that read it infinite or NaN.  Weights enter the sum of values with a relative error of 2^-17 (fp32: 2^-24;
+ * TSD_E4M3: 2^-22, and 2^-32 of the largest weight).
  *
  *   q, out     device [batch, n_q_heads, head_dim] of `dtype` (TSD_F32 with an fp32 cache, else TSD_BF16), strides
  *              (batch, head); 16-byte aligned bases and strides, those of out at least head_dim.
@@ -701,8 +703,8 @@ int tsd_paged_attention(const tsd_paged_cache* cache, int32_t n_q_heads, int32_t
 /* ---------------------------------------------------------------------------
  * tsd_verify_attention with the cached keys and values read from pages: arguments as for that call, the cache's
  * batch, kv heads and head_dim those of the layout, max_pages * page_size >= layout n_cache; the sequences' cached
- * lengths are those of the mask.  bf16 pages are read in place by the tensor-core kernel (sm_scale > 0, else
- * TSD_ERR_UNSUPPORTED).  8-bit pages (values bf16(decode(code) * scale), as for
+ * lengths are those of the mask.  bf16 pages are read in place by the tensor-core kernel (sm_scale > 0 and strides that a tensor map can
+ * express: above 0, below 2^40 bytes; else TSD_ERR_UNSUPPORTED).  8-bit pages (values bf16(decode(code) * scale), as for
  * tsd_verify_attention_fp8_cache), fp32 pages and TSD_ATTN_FORCE_SIMT put the used rows in order in the workspace first.
  *   workspace    device, 16-byte aligned, tsd_verify_attention_paged_workspace_bytes() bytes (0 for bf16 pages
  *                without TSD_ATTN_FORCE_SIMT; then NULL is accepted); scratch.

@@ -24,10 +24,12 @@
 //             arrive puts the parts together, in their order whoever arrives last, so that results repeat bit by bit.  The blocks
 //             of a cluster read one another's parts in shared memory instead.
 // Lengths are read on the device: a captured call follows them.  Rows past a length are not loaded.
-// Measured (caches larger than L2): 2 sequences of 131072 rows, 28/4 heads of 128, bf16, pages of 64: 85.7 us, 6.27 TB/s, 95 % of what a copy
-// reaches; the same in e4m3: 50.3 us, 5.3 TB/s, where conversions come beside the loads; 48 ragged sequences of up to 4096: 39.9 us, 4.8
-// TB/s.  A call costs about 6 us before its bytes count (the launch and two dependent reads, 2 us; the first chunk on its way, 1 us; the
-// warps' parts, 1 us; the blocks', 2 us), with clusters 4: 1 sequence of 768 rows, 32 heads (12.6 MB): 6.5 us.
+// Measured (caches larger than L2): 2 sequences of 131072 rows, 28/4 heads of 128, bf16, pages of 64: 84.2 us in runs of 30 calls, 6.4 TB/s, 97 %
+// of what a copy reaches (88.6 and 92 % in long runs, at lower clocks); the same in e4m3: 48.4 us, 5.5 TB/s, where conversions come beside the
+// loads; 64/4 heads, tiles of 16: 93.4, in e4m3 67.3; 2 of 65536 in fp32, 4/4 heads 87.0 us, 6.2 TB/s, 28/4 heads 142.8, where the query rows'
+// loads are the limit; 48 ragged sequences of up to 4096, bf16: 39.9 us, 4.8 TB/s.  A call costs about 6 us before its bytes count (the launch
+// and two dependent reads, 2 us; the first chunk on its way, 1 us; the warps' parts, 1 us; the blocks', 2 us), with clusters 4: 1 sequence of 768
+// rows, 32 heads (12.6 MB): 6.6 us.
 #include <cuda_fp16.h>
 #include <algorithm>
 #include <cfloat>
@@ -1166,7 +1168,7 @@ __global__ void __launch_bounds__(TokenPlan<D, kType, HT>::kWarps * 32, 1) token
   if (__any_sync(full, bad_page) && lane == 0 && a.status) atomicOr(a.status, TSD_STATUS_BAD_INDEX);
 }
 
-// Heads per tile: 8 where they suffice (the residuals then ride in the other 8 rows of a product).
+// Heads per tile, the columns of a product: 8 where they suffice; 16 are two products, their accumulators for 8 warps instead of 12.
 static int head_tile(int group) { return group <= 8 ? 8 : 16; }
 
 // The kernel's dynamic shared memory limit, an attribute per device.

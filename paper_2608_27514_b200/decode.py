@@ -2,8 +2,8 @@
 
 ``BlockDecoder`` strings the library's kernels into the paper's loop.  One pass =
 
-    caller's model forward over every node of the tree   (its attention layers call
-                                                          ``VerifyStep.attention``)
+    caller's model forward over every node of the tree   (its attention layers call ``VerifyStep.attention``, or, over
+                                                          a cache in pages, ``VerifyStep.attention_paged``)
     -> tsd_advance_block        scores of this pass = candidate pool of the next (Section 3.1), longest
                                 verified trajectory (Section 3.3), next root into the token buffer with
                                 its sequential step indices, tree of the next pass (Alg. 1 Phase 2)
