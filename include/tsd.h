@@ -703,8 +703,8 @@ int tsd_paged_attention(const tsd_paged_cache* cache, int32_t n_q_heads, int32_t
 /* ---------------------------------------------------------------------------
  * tsd_verify_attention with the cached keys and values read from pages: arguments as for that call, the cache's
  * batch, kv heads and head_dim those of the layout, max_pages * page_size >= layout n_cache; the sequences' cached
- * lengths are those of the mask.  bf16 pages are read in place by the tensor-core kernel (sm_scale > 0 and strides that a tensor map can
- * express: above 0, below 2^40 bytes; else TSD_ERR_UNSUPPORTED).  8-bit pages (values bf16(decode(code) * scale), as for
+ * lengths are those of the mask.  bf16 pages are read in place by the tensor-core kernel (sm_scale > 0 and strides below 2^40 bytes, as a
+ * tensor map has them; else TSD_ERR_UNSUPPORTED).  8-bit pages (values bf16(decode(code) * scale), as for
  * tsd_verify_attention_fp8_cache), fp32 pages and TSD_ATTN_FORCE_SIMT put the used rows in order in the workspace first.
  *   workspace    device, 16-byte aligned, tsd_verify_attention_paged_workspace_bytes() bytes (0 for bf16 pages
  *                without TSD_ATTN_FORCE_SIMT; then NULL is accepted); scratch.

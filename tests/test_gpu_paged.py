@@ -831,6 +831,102 @@ def test_arguments_of_an_append_that_do_not_convert():
     assert bool((out == 7).all())
 
 
+def test_a_captured_verification_follows_lengths_and_table():
+    # one graph of a mask and a pass over pages, replayed while sequences grow and their pages change
+    S, Bn, R, Hq, Hkv, d, page, Nc = 2, 3, 32, 8, 2, 128, 16, 320
+    for kind in ("bf16", "e4m3"):
+        pool = Pool(kind, [Nc] * S, Hkv, d, page, seed=7)
+        gen = torch.Generator(device=DEV).manual_seed(8)
+        q, kd, vd = [_rnd(gen, S, Bn * R, h, d, dtype=torch.bfloat16) for h in (Hq, Hkv, Hkv)]
+        steps = [VerifyStep(S, Bn, R, Nc, Hq, Hkv, d, 64, 1, torch.bfloat16) for _ in range(2)]
+        lens = _i32([100, 0])
+
+        def layer(st):
+            st.build_mask(None, lens)
+            return st.attention_paged(q, pool.cache, kd, vd, 0.09)
+
+        stream = torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(stream):
+            layer(steps[0])
+            stream.synchronize()
+            with torch.cuda.graph(graph, stream=stream):
+                layer(steps[0])
+            for n in ([320, 1], [64, 65], [0, 319], [0, 0]):
+                lens.copy_(_i32(n))
+                pool.table.copy_(pool.table[:, torch.randperm(pool.table.shape[1], generator=gen, device=DEV)])
+                steps[0].out.fill_(5.0)
+                graph.replay()
+                layer(steps[1])
+                assert torch.equal(steps[0].out, steps[1].out) and torch.equal(steps[0].attn_lse, steps[1].attn_lse)
+                for s in range(S):
+                    keys, values = pool.dense("k", s, n[s]), pool.dense("v", s, n[s])
+                    kk, vv = np.concatenate([keys, _np(kd[s, :R])]), np.concatenate([values, _np(vd[s, :R])])
+                    ref, _ = oracle.token_attention(_np(q[s, 5]), kk, vv, 0.09)
+                    # cached values and weights in bf16, half a step each, and the output's own
+                    assert np.abs(_np(steps[0].out[s, 5]) - ref).max() <= 3 * 2.0 ** -8 * np.abs(vv).max()
+            stream.synchronize()
+        for st in steps:
+            st.check_status()
+
+
+def test_graphs_that_share_a_workspace_and_a_stream_of_the_call():
+    # graphs of different shapes, replayed in turn on one stream with one workspace; eager calls on a stream that is not the current one
+    lens = [[900, 33, 0], [4000]]
+    pools = [Pool("bf16", lens[0], 4, 128, 16, seed=1), Pool("e4m3", lens[1], 2, 64, 64, seed=2)]
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    qs = [_rnd(gen, 3, 28, 128, dtype=torch.bfloat16), _rnd(gen, 1, 40, 64, dtype=torch.bfloat16)]
+    ws = torch.zeros(max(B.tsd_paged_attention_workspace_bytes(p.cache, q.shape[1]) for p, q in zip(pools, qs)), dtype=torch.uint8, device=DEV)
+    alone = [_token(p, q, _i32(n), 0.09)[:2] for p, q, n in zip(pools, qs, lens)]
+    lt, outs, lses = [_i32(n) for n in lens], [torch.empty_like(q) for q in qs], [torch.empty(q.shape[:2], device=DEV) for q in qs]
+    graphs, stream = [torch.cuda.CUDAGraph() for _ in pools], torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def call(i, where=None):
+        B.tsd_paged_attention(pools[i].cache, qs[i], lt[i], outs[i], lses[i], 0.09, ws, stream=where)
+
+    for i in range(2):                                                                  # given by its object and by its number
+        call(i, (stream, stream.cuda_stream)[i])
+    stream.synchronize()
+    for i in range(2):
+        assert torch.equal(outs[i], alone[i][0]) and torch.equal(lses[i], alone[i][1])
+    with torch.cuda.stream(stream):
+        for i in range(2):
+            with torch.cuda.graph(graphs[i], stream=stream):
+                call(i)
+        for turn in range(20):
+            for i in range(2):
+                outs[i].fill_(1.0)
+                graphs[i].replay()
+                assert torch.equal(outs[i], alone[i][0]) and torch.equal(lses[i], alone[i][1])
+    assert not ws[:148 * 4].any()
+
+
+def test_shared_pages_and_broadcast_queries():
+    # sequences that begin alike share pages, a page may stand twice in a table; one query for all sequences has a stride of 0
+    pool = Pool("bf16", [200, 200, 200], 2, 128, 16, seed=4)
+    pool.table[1, :8], pool.table[2] = pool.table[0, :8], pool.table[0, 3]
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    q = torch.nn.Parameter(_rnd(gen, 1, 8, 128, dtype=torch.bfloat16))
+    lens = [200, 190, 77]
+    out, lse, status = _token(pool, q.expand(3, -1, -1), _i32(lens), 0.09, out=torch.empty((3, 8, 128), dtype=torch.bfloat16, device=DEV))
+    assert status.item() == 0
+    _check_token(pool, q.detach().expand(3, -1, -1), lens, out, lse, 0.09)
+
+
+@pytest.mark.parametrize("flags", [0, B.TSD_ATTN_FORCE_SIMT])
+def test_a_verification_of_one_query_row_for_every_node(flags):
+    # rows with a stride of 0, over bf16 pages too: the bits of the same rows laid out
+    pool = Pool("bf16", [64], 2, 128, 16)
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    row, kd = _rnd(gen, 1, 1, 4, 128, dtype=torch.bfloat16), _rnd(gen, 1, 32, 2, 128, dtype=torch.bfloat16)
+    step = VerifyStep(1, 1, 32, 64, 4, 2, 128, 64, 1, torch.bfloat16)
+    a = step.attention_paged(row.expand(-1, 32, -1, -1), pool.cache, kd, kd, 0.1, flags).clone()
+    assert torch.equal(a, step.attention_paged(row.expand(-1, 32, -1, -1).contiguous(), pool.cache, kd, kd, 0.1, flags))
+    step.check_status()
+
+
 # ---------------------------------------------------------------------------------------- together
 def test_a_block_from_prompt_to_next_token():
     """Prompts into pages, a tree's rows rotated, verified over the pages, its accepted node appended, and a token on top: every stage
